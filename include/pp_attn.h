@@ -227,6 +227,102 @@ int pp_preference_loss(const pp_plan* plan, const float* token_logp, const float
                        float* d_token_logp, pp_stream_t stream);
 
 /*
+ * The steps of a training step on image prompts and on rewards, around the same packed layout.  All of them
+ * need only a plan for the same descriptors, are one kernel on `stream`, and take DEVICE
+ * pointers; results do not depend on the order in which blocks run.
+ *
+ * Position ids with a time, a height and a width axis (the paper trains on image prompts, Sec. 4).  A
+ * token of text has the running number n of its unpacked sequence (x, y^k) on all three axes.  Image and video tokens
+ * come in spans: span i is the span_grid[i] = (f, h, w) consecutive tokens from packed token
+ * span_start[i] on, frame by frame and row by row; if it starts at number n, its tokens are at
+ * (n + frame, n + row, n + column) and what follows goes on at n + max(f, h, w).  Every response goes on
+ * where its prompt ends.
+ *   in : span_start [num_spans] ascending, span_grid [num_spans][3] (int32; may be NULL without spans).  A span lies
+ *        inside one segment (a prompt or a response); spans do not overlap
+ *   out: position_ids [3][T] (int32); status [2]: 0 = fine, 1 = a span breaks these rules, and status[1] = the
+ *        first such span (the positions of its group's tokens are then undefined)
+ *
+ * Rotary embedding by axes (rotate-half form): frequency i of head_dim / 2 turns by
+ * position_ids[axis_of_freq[i]][t] * rope_base^(-2i/D).  axis_of_freq: HOST array of head_dim / 2 entries below
+ * num_axes (1 .. 4), read during the call.  position_ids [num_axes][T] may be of any sign and size; the angle
+ * is reduced without rounding.  q, k are read and q_out, k_out written, bf16 with the heads
+ * of a token side by side ([T][H][D] with strides of *_stride elements between tokens, multiples of 8, at least H * D), so that
+ * they may lie in the buffer of a fused projection; in place where the output is the input
+ * (same pointer and stride); otherwise they must not overlap.  inverse != 0 turns the other
+ * way, which is the backward pass: dQ and dK in, the gradients of what was rotated out.
+ */
+int pp_position_ids_axes(const pp_plan* plan, int32_t num_spans, const int32_t* span_start,
+                         const int32_t* span_grid, int32_t* position_ids, int32_t* status,
+                         pp_stream_t stream);
+int pp_rope_qk_axes(const pp_plan* plan, const void* q, int64_t q_stride, const void* k,
+                    int64_t k_stride, void* q_out, int64_t q_out_stride, void* k_out,
+                    int64_t k_out_stride, const int32_t* position_ids, int32_t num_axes,
+                    const uint8_t* axis_of_freq, float rope_base, int32_t inverse,
+                    pp_stream_t stream);
+
+/*
+ * Log-probabilities of the packed tokens, what the losses below and above take as token_logp.
+ * logits [T][vocab] (bf16, fp16 or fp32, row_stride >= vocab elements between rows) are those of the packed rows; the row
+ * that predicts a token is the one before it, and for the first token of EVERY response of a
+ * group the prompt's last row (Sec. 3.2: the responses share the prompt).  With x = logits / temperature:
+ *   token_logp [T]     x[y_t] - m - l of the response tokens; 0 for prompt tokens and for tokens whose
+ *                      id is negative (not learned); NaN where the id is >= vocab
+ *   row_stats [T][2]   (m, l) of each row that predicts a token: m = max x, l = log sum exp(x - m);
+ *                      (0, 0) for the others, which are not read
+ * token_ids [T]: int32, or int64 with ids_are_64 != 0.  Logits of -inf are ids that cannot be sampled; a row
+ * that is all -inf, or holds +inf or NaN, has NaN log-probabilities.
+ *
+ * pp_token_logp_bwd: the gradient of the logits for given d_token_logp [T] (fp32; entries of prompt
+ * tokens and of tokens with a negative id do not count), in the logits' type:
+ *   d_logits[r][v] = sum over the tokens t that row r predicts of d_token_logp[t] * (1[v = y_t] - p_r(v)) / temperature
+ * Every row is written; a row that predicts nothing, or whose tokens' gradients are all zero, is
+ * not read and gets zeros.  d_logits may be logits (same pointer and stride).  token_logp and
+ * row_stats are those of the forward call with the same logits, ids and temperature.
+ * Both leave what lies between vocab and the stride as it is.  16-byte loads where rows of logits and of
+ * d_logits start alike to 16 bytes, element by element otherwise.
+ */
+enum pp_dtype { PP_BF16 = 0, PP_FP16 = 1, PP_FP32 = 2 };
+int pp_token_logp(const pp_plan* plan, const void* logits, int32_t logits_type, int64_t row_stride,
+                  int32_t vocab, const void* token_ids, int32_t ids_are_64, float temperature,
+                  float* token_logp, float* row_stats, pp_stream_t stream);
+int pp_token_logp_bwd(const pp_plan* plan, const void* logits, int32_t logits_type,
+                      int64_t row_stride, int32_t vocab, const void* token_ids, int32_t ids_are_64,
+                      float temperature, const float* token_logp, const float* row_stats,
+                      const float* d_token_logp, void* d_logits, int64_t d_row_stride,
+                      pp_stream_t stream);
+
+/*
+ * Clipped policy loss with a KL term over the responses, and its gradient.  (The paper's losses, Sec. 2.1, are
+ * pairwise; policy training samples the same groups, a prompt and its responses.)
+ *   A      advantage: of response k from reward [N] (as given, less its group's mean, or that over its group's
+ *          standard deviation, n - 1 in the denominator, + eps; 0 in a group of one), or per token from reward [T]
+ *   rho_t  exp(token_logp - old_token_logp); 1 without old_token_logp (NULL)
+ *   l_t    -min(rho_t A, clip(rho_t, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(d_t) - d_t - 1),
+ *          d_t = ref_token_logp - token_logp; no such term without ref_token_logp (NULL)
+ * over the tokens of response k whose token_mask [T] (one byte; NULL: all) is not zero, n_k of them:
+ *   resp_loss [N]      w_k sum l_t, w_k = scale / n_k (PP_REDUCE_RESPONSE) or scale (PP_REDUCE_TOKEN): the loss is
+ *                      their sum, a mean with scale = 1 / responses or 1 / tokens of the whole batch
+ *   resp_kl [N]        mean of exp(d_t) - d_t - 1          resp_clipped [N]  share of tokens at a clipped border
+ *   advantage [N]      A (may be NULL; not written with PP_ADVANTAGE_TOKEN)
+ *   d_token_logp [T]   d(sum of resp_loss) / d token_logp (may be NULL); 0 for prompt and masked tokens
+ * A response without unmasked tokens has zeros.  What masked and prompt entries hold does not matter.
+ */
+enum pp_advantage { PP_ADVANTAGE_GIVEN = 0, PP_ADVANTAGE_CENTERED = 1, PP_ADVANTAGE_NORMALIZED = 2, PP_ADVANTAGE_TOKEN = 3 };
+enum pp_reduction { PP_REDUCE_RESPONSE = 0, PP_REDUCE_TOKEN = 1 };
+typedef struct {
+  int32_t advantage_mode;      /* pp_advantage */
+  int32_t reduction;           /* pp_reduction */
+  double clip_low, clip_high;  /* 0 <= clip_low <= 1, 0 <= clip_high */
+  double kl_coef;              /* >= 0 */
+  double scale;
+  double eps;                  /* > 0 */
+} pp_policy;
+int pp_policy_loss(const pp_plan* plan, const pp_policy* policy, const float* token_logp,
+                   const float* old_token_logp, const float* ref_token_logp, const float* reward,
+                   const uint8_t* token_mask, float* advantage, float* resp_loss, float* resp_kl,
+                   float* resp_clipped, float* d_token_logp, pp_stream_t stream);
+
+/*
  * pp_attn_bwd for callers that cannot allocate device memory.  (The paper has no counterpart:
  * this is a packaging variant of the backward above, not a different computation.)
  *

@@ -11,6 +11,7 @@ pp_attn_bwd.
 from __future__ import annotations
 
 import ctypes
+import functools
 import importlib
 import os
 from typing import Optional, Sequence, Tuple
@@ -33,6 +34,7 @@ EXPORTS = ["pp_plan_workspace_bytes", "pp_build_plan", "pp_plan_status", "pp_des
            "pp_plan_read_bwd_sched", "pp_plan_read_fwd_units", "pp_plan_read_bwd_tiles", "pp_attn_bwd_deterministic",
            "pp_position_ids", "pp_rope_qk", "pp_preference_loss",
            "pp_build_rows_workspace_bytes", "pp_build_rows", "pp_assign_rows",
+           "pp_position_ids_axes", "pp_rope_qk_axes", "pp_token_logp", "pp_token_logp_bwd", "pp_policy_loss",
            "pp_debug_expire_wait"]
 
 
@@ -94,6 +96,13 @@ def lib() -> ctypes.CDLL:
         L.pp_position_ids.argtypes = [vp, vp, vp]
         L.pp_rope_qk.argtypes = [vp, vp, vp, ctypes.c_float, vp]
         L.pp_preference_loss.argtypes = [vp, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp]
+        L.pp_position_ids_axes.argtypes = [vp, ctypes.c_int32, vp, vp, vp, vp, vp]
+        L.pp_rope_qk_axes.argtypes = [vp] + [vp, ctypes.c_int64] * 4 + [vp, ctypes.c_int32, vp, ctypes.c_float,
+                                                                        ctypes.c_int32, vp]
+        logits = [vp, vp, ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, vp, ctypes.c_int32, ctypes.c_float]
+        L.pp_token_logp.argtypes = logits + [vp, vp, vp]
+        L.pp_token_logp_bwd.argtypes = logits + [vp, vp, vp, vp, ctypes.c_int64, vp]
+        L.pp_policy_loss.argtypes = [vp] * 13
         L.pp_profile_enable.argtypes = [ctypes.c_int]
         L.pp_profile_read.argtypes = [vp, vp]
         L.pp_profile_read_all.argtypes = [vp, vp, ctypes.c_int32, vp, vp]
@@ -355,6 +364,84 @@ def pp_preference_loss(plan: Plan, token_logp: torch.Tensor, ref_token_logp: Opt
           float(beta), resp_logp.data_ptr(), resp_reward.data_ptr(), grp_loss.data_ptr(),
           grad.data_ptr() if want_grad else None)
     return resp_logp, resp_reward, grp_loss, grad
+
+
+def pp_position_ids_axes(plan: Plan, span_start: torch.Tensor, span_grid: torch.Tensor,
+                         out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Packed position ids with a time, a height and a width axis.  Image and video tokens come in
+    spans: ``span_start`` [I] their first packed tokens, ascending, ``span_grid`` [I, 3] their (frames, height, width),
+    int32 DEVICE tensors.  Returns (position_ids [3, T] int32, status [2] int32); a ``status[0]`` of 1
+    says that span ``status[1]`` does not lie inside one segment or overlaps the one before it."""
+    return _step_calls().position_ids_axes(plan.handle, plan.workspace, plan.total_tokens, int(span_start.numel()),
+                                           span_start, span_grid, out)
+
+
+@functools.lru_cache(maxsize=64)
+def axis_of_frequency(sections: Tuple[int, ...], interleaved: bool = False) -> bytes:
+    """Which axis each of the sum(sections) frequencies turns by: the axes' shares one after the other, or
+    (``interleaved``) in turns until an axis has had its share."""
+    if not 1 <= len(sections) <= 4 or min(sections) < 0:
+        raise ValueError(f"sections: expected the frequencies of 1 to 4 axes, got {sections}")
+    if not interleaved:
+        return bytes(a for a, n in enumerate(sections) for _ in range(n))
+    return bytes(a for i in range(max(sections)) for a, n in enumerate(sections) if i < n)
+
+
+def pp_rope_qk_axes(plan: Plan, q: torch.Tensor, k: torch.Tensor, position_ids: torch.Tensor,
+                    sections: Sequence[int], rope_base: float = 10000.0, interleaved: bool = False,
+                    inverse: bool = False, q_out: Optional[torch.Tensor] = None,
+                    k_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Rotary embedding of q [T,Hq,D] and k [T,Hkv,D] by ``position_ids`` [axes, T] int32, in place or into
+    ``q_out`` / ``k_out``; q, k and the outputs may be views of a fused projection's buffer.
+    ``sections``: how many of the D / 2 frequencies each axis has (see ``axis_of_frequency``).
+    ``inverse``: the backward pass, on dQ and dK.  Returns (q_out, k_out)."""
+    axis = axis_of_frequency(tuple(sections), bool(interleaved))
+    handle, T, Hq, Hkv, D = plan._head
+    return _step_calls().rope_qk_axes(handle, plan.workspace, T, Hq, Hkv, D, q, k, position_ids, len(sections), axis,
+                                      rope_base, inverse, q_out, k_out)
+
+
+def pp_token_logp(plan: Plan, logits: torch.Tensor, token_ids: torch.Tensor, temperature: float = 1.0,
+                  token_logp: Optional[torch.Tensor] = None, row_stats: Optional[torch.Tensor] = None):
+    """Log-probabilities of the packed response tokens from ``logits`` [T, V] (bf16, fp16 or fp32; adjacent columns)
+    under ``token_ids`` [T] (int32 or int64, negative: not learned).  The first token of every response is
+    predicted by the prompt's last row.  Returns (token_logp [T], row_stats [T, 2]), both fp32; ``row_stats``
+    is for the backward pass."""
+    return _step_calls().token_logp(plan.handle, plan.workspace, plan.total_tokens, logits, token_ids, temperature,
+                                    token_logp, row_stats)
+
+
+def pp_token_logp_bwd(plan: Plan, logits: torch.Tensor, token_ids: torch.Tensor, token_logp: torch.Tensor,
+                      row_stats: torch.Tensor, d_token_logp: torch.Tensor, temperature: float = 1.0,
+                      d_logits: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of the logits, given that of the log-probabilities; ``d_logits`` may be ``logits``, a new one has
+    the row stride of ``logits``."""
+    return _step_calls().token_logp_bwd(plan.handle, plan.workspace, plan.total_tokens, logits, token_ids, token_logp,
+                                        row_stats, d_token_logp, temperature, d_logits)
+
+
+_ADVANTAGES = {"given": 0, "centered": 1, "normalized": 2, "token": 3}
+_REDUCTIONS = {"response": 0, "token": 1}
+
+
+def pp_policy_loss(plan: Plan, token_logp: torch.Tensor, old_token_logp: Optional[torch.Tensor],
+                   ref_token_logp: Optional[torch.Tensor], reward: torch.Tensor, advantage: str = "normalized",
+                   token_mask: Optional[torch.Tensor] = None, clip_low: float = 0.2, clip_high: float = 0.2,
+                   kl_coef: float = 0.0, reduction: str = "response", scale: float = 1.0, eps: float = 1e-6,
+                   want_grad: bool = True):
+    """Clipped policy loss with a KL term over the responses.  ``advantage``: of a response from ``reward`` [N]
+    ("given", "centered" on its group's mean, "normalized" also by the group's standard deviation) or of a token
+    ("token", reward [T]).  ``token_mask`` [T] bool.  ``reduction``: mean over a response's tokens ("response") or
+    sum ("token"), times ``scale``.  Returns (resp_loss [N], resp_kl [N], resp_clipped [N], advantage [N] or None,
+    d_token_logp [T] or None); the loss is resp_loss.sum()."""
+    if advantage not in _ADVANTAGES:
+        raise ValueError(f"advantage: expected one of {', '.join(_ADVANTAGES)}, got {advantage!r}")
+    if reduction not in _REDUCTIONS:
+        raise ValueError(f"reduction: expected one of {', '.join(_REDUCTIONS)}, got {reduction!r}")
+    return _step_calls().policy_loss(plan.handle, plan.workspace, plan.total_tokens, plan.problem.num_responses,
+                                     token_logp, old_token_logp, ref_token_logp, reward, token_mask,
+                                     _ADVANTAGES[advantage], _REDUCTIONS[reduction], clip_low, clip_high, kl_coef,
+                                     scale, eps, want_grad)
 
 
 def pp_attn_bwd_noalloc_max_bytes() -> int:

@@ -12,8 +12,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpp_attn.so")
 EXT_SOURCE = "pp_torch.cpp"
-SOURCES = ["pp_api.cu", "pp_plan.cu", "pp_fwd.cu", "pp_bwd.cu", "pp_rope.cu", "pp_loss.cu", "pp_rows.cu"]
-HEADERS = ["pp_internal.h", "pp_dev.cuh", "pp_ptx.cuh", os.path.join("..", "..", "include", "pp_attn.h")]
+SOURCES = ["pp_api.cu", "pp_plan.cu", "pp_fwd.cu", "pp_bwd.cu", "pp_rope.cu", "pp_loss.cu", "pp_rows.cu",
+           "pp_logp.cu", "pp_policy.cu", "pp_axes.cu"]
+HEADERS = ["pp_internal.h", "pp_dev.cuh", "pp_ptx.cuh", "pp_seg.cuh", os.path.join("..", "..", "include", "pp_attn.h")]
 
 
 def _nvcc() -> str:

@@ -414,6 +414,104 @@ int pp_preference_loss(const pp_plan* plan, const float* token_logp, const float
   return PP_OK;
 }
 
+int pp_position_ids_axes(const pp_plan* plan, int32_t num_spans, const int32_t* span_start, const int32_t* span_grid,
+                         int32_t* position_ids, int32_t* status, pp_stream_t stream) {
+  g_last_launches = 0;
+  if (!plan || !position_ids || !status || num_spans < 0) return PP_ERR_INVALID_ARG;
+  if (num_spans && (!span_start || !span_grid)) return PP_ERR_INVALID_ARG;
+  if (pp::launch_position_ids_axes(plan, num_spans, span_start, span_grid, position_ids, status,
+                                   reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess)
+    return PP_ERR_CUDA;
+  g_last_launches = 1;
+  return PP_OK;
+}
+
+int pp_rope_qk_axes(const pp_plan* plan, const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out,
+                    int64_t q_out_stride, void* k_out, int64_t k_out_stride, const int32_t* position_ids,
+                    int32_t num_axes, const uint8_t* axis_of_freq, float rope_base, int32_t inverse,
+                    pp_stream_t stream) {
+  g_last_launches = 0;
+  if (!plan || !q || !k || !q_out || !k_out || !position_ids || !axis_of_freq) return PP_ERR_INVALID_ARG;
+  if (num_axes < 1 || num_axes > 4) return PP_ERR_INVALID_ARG;
+  if (!(rope_base > 1.f) || rope_base > 1e12f) return PP_ERR_INVALID_ARG;
+  const pp_problem& p = plan->prob;
+  for (int i = 0; i < p.head_dim / 2; ++i)
+    if (axis_of_freq[i] >= num_axes) return PP_ERR_INVALID_ARG;
+  const int64_t qd = int64_t(p.num_q_heads) * p.head_dim, kd = int64_t(p.num_kv_heads) * p.head_dim;
+  if (q_stride < qd || q_out_stride < qd || k_stride < kd || k_out_stride < kd) return PP_ERR_INVALID_ARG;
+  if (q_out == q && q_out_stride != q_stride) return PP_ERR_INVALID_ARG;
+  if (k_out == k && k_out_stride != k_stride) return PP_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) ||
+      ((q_stride | k_stride | q_out_stride | k_out_stride) & 7))
+    return PP_ERR_ALIGNMENT;
+  if (pp::launch_rope_axes(plan, q, q_stride, k, k_stride, q_out, q_out_stride, k_out, k_out_stride, position_ids,
+                           axis_of_freq, rope_base, inverse != 0, reinterpret_cast<cudaStream_t>(stream)) !=
+      cudaSuccess)
+    return PP_ERR_CUDA;
+  g_last_launches = 1;
+  return PP_OK;
+}
+
+static int check_logits(const pp_plan* plan, const void* logits, int32_t type, int64_t row_stride, int32_t vocab,
+                        const void* token_ids, float temperature) {
+  if (!plan || !logits || !token_ids || vocab < 1 || row_stride < vocab) return PP_ERR_INVALID_ARG;
+  if (type < PP_BF16 || type > PP_FP32) return PP_ERR_UNSUPPORTED;
+  if (!(temperature >= 1e-4f) || temperature > 1e4f) return PP_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(logits) & (type == PP_FP32 ? 3 : 1)) return PP_ERR_ALIGNMENT;
+  return PP_OK;
+}
+
+int pp_token_logp(const pp_plan* plan, const void* logits, int32_t logits_type, int64_t row_stride, int32_t vocab,
+                  const void* token_ids, int32_t ids_are_64, float temperature, float* token_logp, float* row_stats,
+                  pp_stream_t stream) {
+  g_last_launches = 0;
+  if (const int rc = check_logits(plan, logits, logits_type, row_stride, vocab, token_ids, temperature)) return rc;
+  if (!token_logp || !row_stats) return PP_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(row_stats) & 7) return PP_ERR_ALIGNMENT;
+  if (pp::launch_token_logp(plan, logits, logits_type, row_stride, vocab, token_ids, ids_are_64 != 0, temperature,
+                            token_logp, row_stats, reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess)
+    return PP_ERR_CUDA;
+  g_last_launches = 1;
+  return PP_OK;
+}
+
+int pp_token_logp_bwd(const pp_plan* plan, const void* logits, int32_t logits_type, int64_t row_stride, int32_t vocab,
+                      const void* token_ids, int32_t ids_are_64, float temperature, const float* token_logp,
+                      const float* row_stats, const float* d_token_logp, void* d_logits, int64_t d_row_stride,
+                      pp_stream_t stream) {
+  g_last_launches = 0;
+  if (const int rc = check_logits(plan, logits, logits_type, row_stride, vocab, token_ids, temperature)) return rc;
+  if (!token_logp || !row_stats || !d_token_logp || !d_logits || d_row_stride < vocab) return PP_ERR_INVALID_ARG;
+  if (d_logits == logits && d_row_stride != row_stride) return PP_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(row_stats) & 7) return PP_ERR_ALIGNMENT;
+  if (reinterpret_cast<uintptr_t>(d_logits) & (logits_type == PP_FP32 ? 3 : 1)) return PP_ERR_ALIGNMENT;
+  if (pp::launch_token_logp_bwd(plan, logits, logits_type, row_stride, vocab, token_ids, ids_are_64 != 0, temperature,
+                                token_logp, row_stats, d_token_logp, d_logits, d_row_stride,
+                                reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess)
+    return PP_ERR_CUDA;
+  g_last_launches = 1;
+  return PP_OK;
+}
+
+int pp_policy_loss(const pp_plan* plan, const pp_policy* policy, const float* token_logp, const float* old_token_logp,
+                   const float* ref_token_logp, const float* reward, const uint8_t* token_mask, float* advantage,
+                   float* resp_loss, float* resp_kl, float* resp_clipped, float* d_token_logp, pp_stream_t stream) {
+  g_last_launches = 0;
+  if (!plan || !policy || !token_logp || !reward || !resp_loss || !resp_kl || !resp_clipped) return PP_ERR_INVALID_ARG;
+  const pp_policy& o = *policy;
+  if (o.advantage_mode < PP_ADVANTAGE_GIVEN || o.advantage_mode > PP_ADVANTAGE_TOKEN) return PP_ERR_INVALID_ARG;
+  if (o.reduction != PP_REDUCE_RESPONSE && o.reduction != PP_REDUCE_TOKEN) return PP_ERR_INVALID_ARG;
+  if (!(o.clip_low >= 0) || o.clip_low > 1 || !(o.clip_high >= 0) || o.clip_high > 1e30) return PP_ERR_INVALID_ARG;
+  if (!(o.kl_coef >= 0) || o.kl_coef > 1e30 || !(o.scale >= -1e30) || o.scale > 1e30) return PP_ERR_INVALID_ARG;
+  if (!(o.eps > 0) || o.eps > 1e30) return PP_ERR_INVALID_ARG;
+  if (pp::launch_policy_loss(plan, o, token_logp, old_token_logp, ref_token_logp, reward, token_mask, advantage,
+                             resp_loss, resp_kl, resp_clipped, d_token_logp,
+                             reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess)
+    return PP_ERR_CUDA;
+  g_last_launches = 1;
+  return PP_OK;
+}
+
 int pp_last_launch_count(void) { return g_last_launches; }
 
 int pp_step_host_arena_bytes(const pp_problem* problem, size_t* arena_bytes) {

@@ -420,4 +420,21 @@ cudaError_t launch_preference_loss(const pp_plan* plan, const float* logp, const
                                    float beta, float* resp_logp, float* resp_reward,
                                    float* grp_loss, float* d_logp, cudaStream_t stream);
 
+cudaError_t launch_token_logp(const pp_plan* plan, const void* logits, int type, long long row_stride, int V,
+                              const void* ids, int ids_64, float temperature, float* logp, float* stats,
+                              cudaStream_t stream);
+cudaError_t launch_token_logp_bwd(const pp_plan* plan, const void* logits, int type, long long row_stride, int V,
+                                  const void* ids, int ids_64, float temperature, const float* logp,
+                                  const float* stats, const float* grad, void* d_logits, long long d_stride,
+                                  cudaStream_t stream);
+cudaError_t launch_policy_loss(const pp_plan* plan, const pp_policy& o, const float* logp, const float* old,
+                               const float* ref, const float* reward, const uint8_t* mask, float* advantage,
+                               float* loss, float* kl, float* clipped, float* d_logp, cudaStream_t stream);
+cudaError_t launch_position_ids_axes(const pp_plan* plan, int num_spans, const int32_t* span_start,
+                                     const int32_t* span_grid, int32_t* pos, int32_t* status, cudaStream_t stream);
+cudaError_t launch_rope_axes(const pp_plan* plan, const void* q, long long q_stride, const void* k, long long k_stride,
+                             void* q_out, long long q_out_stride, void* k_out, long long k_out_stride,
+                             const int32_t* pos, const uint8_t* axis_of_freq, float base, bool inverse,
+                             cudaStream_t stream);
+
 }  // namespace pp

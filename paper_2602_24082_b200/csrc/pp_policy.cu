@@ -1,0 +1,203 @@
+// Clipped policy loss with a KL term over the responses of a packed batch, and its gradient.
+//
+// The packed groups (paper Sec. 3.1: a prompt and its K responses) are what policy training samples; the paper
+// itself trains on pairwise losses, of which this is the sibling for rewards.  Per response k of a group:
+//   A_k    = its reward as given, less the group's mean, or that over the group's standard deviation
+//            (n - 1 in the denominator; 0 for one response) + eps; or one value per token
+//   rho_t  = exp(logp_t - old_t)                          (1 without old log-probabilities)
+//   l_t    = -min(rho_t A, clip(rho_t, 1 - lo, 1 + hi) A) + kl (exp(d) - d - 1),   d = ref_t - logp_t
+//   loss_k = w_k sum_t l_t over the tokens that the mask leaves, w_k = scale / n_k or scale
+//   d logp = w_k ((rho A where rho A <= clip(rho) A, else 0) (-1) + kl (1 - exp(d)))
+// Everything per token is in 64 bits: ratio and border decide whether a token has a gradient at all,
+// and exp(d) - d - 1 is the small difference of large terms near d = 0.  That costs nothing: 16
+// bytes per token make this a kernel of latencies.  So one launch does it all: a team
+// of 1, 2, 4 or 8 warps takes a response, as many as its tokens ask for, or a cluster of up to 8 blocks
+// that add up their sums through distributed shared memory, in the order of their ranks.
+// A prompt's tokens have no gradient; the zeros are written by its responses' teams.
+#include <cooperative_groups.h>
+
+#include "pp_seg.cuh"
+
+namespace pp {
+namespace {
+
+struct PolicyArgs {
+  const int32_t* header;
+  const int32_t* seg_start;
+  const int32_t* grp_resp_off;
+  int G, N;
+  const float *logp, *old, *ref, *reward;
+  const uint8_t* mask;
+  pp_policy o;
+  float *advantage, *loss, *kl, *clipped, *d_logp;
+};
+
+constexpr int kThreads = 256, kMaxParts = 8;
+
+// K sums over a team of kTeam threads of a block, or over all blocks of a cluster (which have started).
+template <int kTeam, int K>
+__device__ __forceinline__ void team_sum(double (&x)[K], double (*buf)[K], double (*slot)[K], int parts) {
+#pragma unroll
+  for (int i = 0; i < K; ++i)
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
+  if constexpr (kTeam > 32) {
+    const int warp = threadIdx.x >> 5, first = warp / (kTeam / 32) * (kTeam / 32);
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+      for (int i = 0; i < K; ++i) buf[warp][i] = x[i];
+    if constexpr (kTeam == kThreads) __syncthreads();
+    else named_barrier_sync(1 + threadIdx.x / kTeam, kTeam);
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      x[i] = 0;
+      for (int w = 0; w < kTeam / 32; ++w) x[i] += buf[first + w][i];
+    }
+  }
+  if constexpr (kTeam == kThreads) {
+    if (parts > 1) {
+      auto cluster = cooperative_groups::this_cluster();
+      if (threadIdx.x < parts)
+#pragma unroll
+        for (int i = 0; i < K; ++i) cluster.map_shared_rank(&slot[cluster.block_rank()][0], int(threadIdx.x))[i] = x[i];
+      cluster.sync();
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        x[i] = 0;
+        for (int b = 0; b < parts; ++b) x[i] += slot[b][i];
+      }
+    }
+  }
+}
+
+template <int kTeam>
+__global__ void __launch_bounds__(kThreads) policy_loss_kernel(PolicyArgs p, int parts) {
+  __shared__ double buf[kThreads / 32][3], count_buf[kThreads / 32][1];
+  __shared__ double slot[kMaxParts][3], count_slot[kMaxParts][1];
+  dependency_wait();
+  if (p.header[0] != kStatusOk) return;
+  const int lane = threadIdx.x & 31, in_team = threadIdx.x % kTeam;
+  const int x = kTeam == kThreads ? blockIdx.x / parts : blockIdx.x * (kThreads / kTeam) + threadIdx.x / kTeam;
+  const int part = kTeam == kThreads ? blockIdx.x % parts : 0;
+  if (x >= p.N) return;
+  if (kTeam == kThreads && parts > 1) cooperative_groups::this_cluster().barrier_arrive();
+  const int g = warp_upper(p.grp_resp_off, p.G, x);
+  const int x0 = p.grp_resp_off[g], n = p.grp_resp_off[g + 1] - x0;
+  const int sp = g + x0, seg = g + 1 + x;
+  const int a = p.seg_start[seg], b = p.seg_start[seg + 1];
+  const int stride = kTeam * parts, first = a + part * kTeam + in_team;
+  if (p.d_logp) {   // this response's share of the prompt's zeros
+    const int p0 = p.seg_start[sp], len = p.seg_start[sp + 1] - p0, j = x - x0;
+    const int lo = p0 + int((long long)len * j / n), hi = p0 + int((long long)len * (j + 1) / n);
+    for (int t = lo + part * kTeam + in_team; t < hi; t += stride) p.d_logp[t] = 0.f;
+  }
+  // the advantage, by every warp for itself
+  double A = 0;
+  if (p.o.advantage_mode != PP_ADVANTAGE_TOKEN) {
+    A = p.reward[x];
+    if (p.o.advantage_mode != PP_ADVANTAGE_GIVEN) {
+      double sum = 0;
+      for (int j = lane; j < n; j += 32) sum += p.reward[x0 + j];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      const double mean = sum / n;
+      A -= mean;
+      if (p.o.advantage_mode == PP_ADVANTAGE_NORMALIZED) {
+        double sq = 0;
+        for (int j = lane; j < n; j += 32) {
+          const double d = p.reward[x0 + j] - mean;
+          sq += d * d;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+        A = n > 1 ? A / (sqrt(sq / (n - 1)) + p.o.eps) : 0.0;
+      }
+    }
+    if (p.advantage && part == 0 && in_team == 0) p.advantage[x] = float(A);
+  }
+  if (kTeam == kThreads && parts > 1) cooperative_groups::this_cluster().barrier_wait();
+  // tokens that count
+  double count = b - a;
+  if (p.mask) {
+    int c = 0;
+#pragma unroll 4
+    for (int t = first; t < b; t += stride) c += p.mask[t] != 0;
+    double n_k[1] = {double(c)};
+    team_sum<kTeam>(n_k, count_buf, count_slot, parts);
+    count = n_k[0];
+  }
+  const double inv = count > 0 ? 1.0 / count : 0.0;
+  const double w = p.o.reduction == PP_REDUCE_RESPONSE ? p.o.scale * inv : p.o.scale;
+  const double low = 1.0 - p.o.clip_low, high = 1.0 + p.o.clip_high;
+  double loss = 0, kl = 0;
+  int clipped = 0;
+#pragma unroll 2
+  for (int t = first; t < b; t += stride) {
+    float d = 0.f;
+    if (!p.mask || p.mask[t]) {
+      const double lp = p.logp[t];
+      const double At = p.o.advantage_mode == PP_ADVANTAGE_TOKEN ? double(p.reward[t]) : A;
+      const double rho = p.old ? exp(lp - double(p.old[t])) : 1.0;
+      // (comparisons, which keep a ratio that is no number)
+      const double u = rho * At, v = (rho < low ? low : rho > high ? high : rho) * At;
+      const bool cut = v < u;
+      double term = cut ? -v : -u, slope = cut ? 0.0 : -u;
+      clipped += cut;
+      if (p.ref) {
+        const double delta = double(p.ref[t]) - lp, e = expm1(delta);
+        kl += e - delta;
+        term += p.o.kl_coef * (e - delta);
+        slope -= p.o.kl_coef * e;
+      }
+      loss += term;
+      d = float(w * slope);
+    }
+    if (p.d_logp) p.d_logp[t] = d;
+  }
+  double sum[3] = {loss, kl, double(clipped)};
+  team_sum<kTeam>(sum, buf, slot, parts);
+  if (part == 0 && in_team == 0) {
+    p.loss[x] = float(w * sum[0]);
+    p.kl[x] = float(inv * sum[1]);
+    p.clipped[x] = float(inv * sum[2]);
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_policy_loss(const pp_plan* plan, const pp_policy& o, const float* logp, const float* old,
+                               const float* ref, const float* reward, const uint8_t* mask, float* advantage,
+                               float* loss, float* kl, float* clipped, float* d_logp, cudaStream_t stream) {
+  static DeviceSetup setup[kMaxDevices];
+  const DeviceSetup* dev = device_setup(setup);
+  if (!dev) return cudaErrorInvalidDevice;
+  PolicyArgs p;
+  p.header = reinterpret_cast<const int32_t*>(plan->ws + plan->lay.header);
+  p.seg_start = reinterpret_cast<const int32_t*>(plan->ws + plan->lay.seg_start);
+  p.grp_resp_off = plan->prob.grp_resp_off;
+  p.G = plan->prob.num_groups;
+  p.N = plan->prob.num_responses;
+  p.logp = logp;
+  p.old = old;
+  p.ref = ref;
+  p.reward = reward;
+  p.mask = mask;
+  p.o = o;
+  p.advantage = advantage;
+  p.loss = loss;
+  p.kl = kl;
+  p.clipped = clipped;
+  p.d_logp = d_logp;
+  // a team's threads take about two tokens of a mean segment each
+  const int mean = plan->prob.total_tokens / plan->nseg;
+  const int N = p.N;
+  if (mean <= 64) return launch_kernel(true, policy_loss_kernel<32>, dim3((N + 7) / 8), dim3(kThreads), 0, stream, p, 1);
+  if (mean <= 128) return launch_kernel(true, policy_loss_kernel<64>, dim3((N + 3) / 4), dim3(kThreads), 0, stream, p, 1);
+  if (mean <= 256) return launch_kernel(true, policy_loss_kernel<128>, dim3((N + 1) / 2), dim3(kThreads), 0, stream, p, 1);
+  int parts = 1;
+  while (parts < kMaxParts && mean > 512 * parts && (long long)N * 2 * parts <= 4ll * dev->num_sms) parts *= 2;
+  return launch_clusters(parts, policy_loss_kernel<kThreads>, dim3(unsigned(N) * parts), dim3(kThreads), 0, stream, p,
+                         parts);
+}
+
+}  // namespace pp

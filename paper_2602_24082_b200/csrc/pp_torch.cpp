@@ -26,6 +26,11 @@ struct Api {
   decltype(&pp_build_rows_workspace_bytes) rows_bytes = nullptr;
   decltype(&pp_build_rows) build_rows = nullptr;
   decltype(&pp_assign_rows) assign_rows = nullptr;
+  decltype(&pp_token_logp) token_logp = nullptr;
+  decltype(&pp_token_logp_bwd) token_logp_bwd = nullptr;
+  decltype(&pp_policy_loss) policy_loss = nullptr;
+  decltype(&pp_position_ids_axes) position_ids_axes = nullptr;
+  decltype(&pp_rope_qk_axes) rope_qk_axes = nullptr;
 } api;
 PyObject* g_error = nullptr;  // PPError(code, where)
 PyObject* g_chk = nullptr;    // _chk(tensor, shape, dtype, name): raises what is wrong with it
@@ -50,12 +55,12 @@ struct Dims {
 // The tensor of `o` if it is a contiguous CUDA tensor of that type and shape, on the device of `on`
 // (if given); otherwise the Python check is called to raise, and null comes back.
 const at::Tensor* take(PyObject* o, at::ScalarType type, const char* type_name, at::IntArrayRef shape,
-                       const char* name, const at::Tensor* on = nullptr) {
+                       const char* name, const at::Tensor* on = nullptr, const char* on_name = "q") {
   if (THPVariable_Check(o)) {
     const at::Tensor& t = THPVariable_Unpack(o);
     if (t.is_cuda() && t.scalar_type() == type && t.sizes() == shape && t.is_contiguous()) {
       if (!on || t.device() == on->device()) return &t;
-      PyErr_Format(PyExc_ValueError, "%s: on another device than q", name);
+      PyErr_Format(PyExc_ValueError, "%s: on another device than %s", name, on_name);
       return nullptr;
     }
   }
@@ -114,7 +119,13 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   x.rows_bytes = reinterpret_cast<decltype(x.rows_bytes)>(dlsym(lib, "pp_build_rows_workspace_bytes"));
   x.build_rows = reinterpret_cast<decltype(x.build_rows)>(dlsym(lib, "pp_build_rows"));
   x.assign_rows = reinterpret_cast<decltype(x.assign_rows)>(dlsym(lib, "pp_assign_rows"));
-  if (!x.build_plan || !x.fwd || !x.bwd || !x.bwd_det || !x.rows_bytes || !x.build_rows || !x.assign_rows) {
+  x.token_logp = reinterpret_cast<decltype(x.token_logp)>(dlsym(lib, "pp_token_logp"));
+  x.token_logp_bwd = reinterpret_cast<decltype(x.token_logp_bwd)>(dlsym(lib, "pp_token_logp_bwd"));
+  x.policy_loss = reinterpret_cast<decltype(x.policy_loss)>(dlsym(lib, "pp_policy_loss"));
+  x.position_ids_axes = reinterpret_cast<decltype(x.position_ids_axes)>(dlsym(lib, "pp_position_ids_axes"));
+  x.rope_qk_axes = reinterpret_cast<decltype(x.rope_qk_axes)>(dlsym(lib, "pp_rope_qk_axes"));
+  if (!x.build_plan || !x.fwd || !x.bwd || !x.bwd_det || !x.rows_bytes || !x.build_rows || !x.assign_rows ||
+      !x.token_logp || !x.token_logp_bwd || !x.policy_loss || !x.position_ids_axes || !x.rope_qk_axes) {
     PyErr_SetString(PyExc_RuntimeError, "libpp_attn.so lacks an entry point");
     return nullptr;
   }
@@ -372,9 +383,237 @@ PyObject* assign_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   PP_GUARD_END
 }
 
+// The steps around the attention.  Every call starts with the plan's handle and its workspace, on whose device
+// all tensors lie.
+struct Around {
+  const pp_plan* plan = nullptr;
+  const at::Tensor* ws = nullptr;
+  bool begin(PyObject* handle, PyObject* workspace) {
+    plan = static_cast<const pp_plan*>(PyLong_AsVoidPtr(handle));
+    return !PyErr_Occurred() && (ws = take_buffer(workspace, "workspace"));
+  }
+  const at::Tensor* take(PyObject* o, at::ScalarType type, const char* type_name, at::IntArrayRef shape,
+                         const char* name) const {
+    return ::take(o, type, type_name, shape, name, ws, "the plan");
+  }
+  // a given output, or a new one
+  bool out(at::Tensor& to, PyObject* o, at::ScalarType type, const char* type_name, at::IntArrayRef shape,
+           const char* name) const {
+    if (o == Py_None) {
+      to = at::empty(shape, ws->options().dtype(type));
+      return true;
+    }
+    const at::Tensor* t = take(o, type, type_name, shape, name);
+    if (t) to = *t;
+    return t != nullptr;
+  }
+  pp_stream_t stream() const { return stream_of(ws->get_device()); }
+};
+
+// position_ids_axes(handle, workspace, T, spans, span_start, span_grid, out | None) -> (position_ids, status)
+PyObject* position_ids_axes(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs(n, 7, "position_ids_axes")) return nullptr;
+  PP_GUARD_BEGIN
+  Around c;
+  if (!c.begin(a[0], a[1])) return nullptr;
+  const int64_t T = PyLong_AsLongLong(a[2]), I = PyLong_AsLongLong(a[3]);
+  if (PyErr_Occurred()) return nullptr;
+  const at::Tensor *start, *grid;
+  if (!(start = c.take(a[4], at::kInt, "int32", {I}, "span_start")) ||
+      !(grid = c.take(a[5], at::kInt, "int32", {I, 3}, "span_grid")))
+    return nullptr;
+  const c10::cuda::CUDAGuard guard(c.ws->device());
+  at::Tensor out;
+  if (!c.out(out, a[6], at::kInt, "int32", {3, T}, "position_ids")) return nullptr;
+  const at::Tensor status = at::empty({2}, start->options());
+  const int rc = api.position_ids_axes(c.plan, int32_t(I), start->data_ptr<int32_t>(), grid->data_ptr<int32_t>(),
+                                       out.data_ptr<int32_t>(), status.data_ptr<int32_t>(), c.stream());
+  if (rc) return raise_code(rc, "pp_position_ids_axes");
+  return Py_BuildValue("(NN)", THPVariable_Wrap(out), THPVariable_Wrap(status));
+  PP_GUARD_END
+}
+
+// A tensor [T][H][D] whose heads lie side by side, whatever lies between tokens.
+const at::Tensor* take_heads(PyObject* o, const Around& c, int64_t T, int64_t H, int64_t D, const char* name) {
+  if (THPVariable_Check(o)) {
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.is_cuda() && t.device() == c.ws->device() && t.scalar_type() == kBf16 && t.dim() == 3 && t.size(0) == T &&
+        t.size(1) == H && t.size(2) == D && t.stride(2) == 1 && (H == 1 || t.stride(1) == D))
+      return &t;
+  }
+  PyErr_Format(PyExc_ValueError, "%s: expected a bfloat16 tensor (%lld, %lld, %lld) with adjacent heads on the plan's device",
+               name, (long long)T, (long long)H, (long long)D);
+  return nullptr;
+}
+int64_t token_stride(const at::Tensor& t) { return t.size(0) == 1 ? t.size(1) * t.size(2) : t.stride(0); }
+
+// rope_qk_axes(handle, workspace, T, Hq, Hkv, D, q, k, position_ids, axes, axis of each frequency (bytes),
+//              base, inverse, q_out | None, k_out | None) -> (q_out, k_out)
+PyObject* rope_qk_axes(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs(n, 15, "rope_qk_axes")) return nullptr;
+  PP_GUARD_BEGIN
+  Around c;
+  if (!c.begin(a[0], a[1])) return nullptr;
+  const int64_t T = PyLong_AsLongLong(a[2]), Hq = PyLong_AsLongLong(a[3]), Hkv = PyLong_AsLongLong(a[4]),
+                D = PyLong_AsLongLong(a[5]), axes = PyLong_AsLongLong(a[9]);
+  const double base = PyFloat_AsDouble(a[11]);
+  const int inverse = PyObject_IsTrue(a[12]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!PyBytes_Check(a[10]) || PyBytes_GET_SIZE(a[10]) != D / 2) {
+    PyErr_SetString(PyExc_ValueError, "rope_qk_axes: expected an axis for each of head_dim / 2 frequencies");
+    return nullptr;
+  }
+  const at::Tensor *q, *k, *pos, *qo, *ko;
+  if (!(q = take_heads(a[6], c, T, Hq, D, "q")) || !(k = take_heads(a[7], c, T, Hkv, D, "k")) ||
+      !(pos = c.take(a[8], at::kInt, "int32", {axes, T}, "position_ids")))
+    return nullptr;
+  if (!(qo = a[13] == Py_None ? q : take_heads(a[13], c, T, Hq, D, "q_out")) ||
+      !(ko = a[14] == Py_None ? k : take_heads(a[14], c, T, Hkv, D, "k_out")))
+    return nullptr;
+  const c10::cuda::CUDAGuard guard(c.ws->device());
+  const int rc = api.rope_qk_axes(c.plan, q->data_ptr(), token_stride(*q), k->data_ptr(), token_stride(*k),
+                                  qo->data_ptr(), token_stride(*qo), ko->data_ptr(), token_stride(*ko),
+                                  pos->data_ptr<int32_t>(), int32_t(axes),
+                                  reinterpret_cast<const uint8_t*>(PyBytes_AS_STRING(a[10])), float(base), inverse,
+                                  c.stream());
+  if (rc) return raise_code(rc, "pp_rope_qk_axes");
+  return Py_BuildValue("(NN)", THPVariable_Wrap(*qo), THPVariable_Wrap(*ko));
+  PP_GUARD_END
+}
+
+// Logits [T][V], or a gradient of them, with adjacent columns.
+const at::Tensor* take_logits(PyObject* o, const Around& c, int64_t T, const at::Tensor* like, const char* name) {
+  if (THPVariable_Check(o)) {
+    const at::Tensor& t = THPVariable_Unpack(o);
+    const auto type = t.scalar_type();
+    if (t.is_cuda() && t.device() == c.ws->device() && (type == kBf16 || type == at::kHalf || type == kF32) &&
+        t.dim() == 2 && t.size(0) == T && t.size(1) >= 1 && t.size(1) <= INT32_MAX &&
+        (t.size(1) == 1 || t.stride(1) == 1) && (T == 1 || t.stride(0) >= t.size(1)) &&
+        (!like || (type == like->scalar_type() && t.size(1) == like->size(1))))
+      return &t;
+  }
+  PyErr_Format(PyExc_ValueError, "%s: expected a bfloat16, float16 or float32 tensor (%lld, vocabulary) with adjacent "
+               "columns on the plan's device%s", name, (long long)T, like ? ", of the logits' type and size" : "");
+  return nullptr;
+}
+int32_t dtype_of(const at::Tensor& t) {
+  return t.scalar_type() == kBf16 ? PP_BF16 : t.scalar_type() == at::kHalf ? PP_FP16 : PP_FP32;
+}
+int64_t row_stride(const at::Tensor& t) { return t.size(0) == 1 ? t.size(1) : t.stride(0); }
+const at::Tensor* take_ids(PyObject* o, const Around& c, int64_t T) {
+  const bool wide = THPVariable_Check(o) && THPVariable_Unpack(o).scalar_type() == at::kLong;
+  return c.take(o, wide ? at::kLong : at::kInt, wide ? "int64" : "int32", {T}, "token_ids");
+}
+
+// token_logp(handle, workspace, T, logits, token_ids, temperature, token_logp | None, row_stats | None)
+//   -> (token_logp, row_stats)
+PyObject* token_logp(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs(n, 8, "token_logp")) return nullptr;
+  PP_GUARD_BEGIN
+  Around c;
+  if (!c.begin(a[0], a[1])) return nullptr;
+  const int64_t T = PyLong_AsLongLong(a[2]);
+  const double temperature = PyFloat_AsDouble(a[5]);
+  if (PyErr_Occurred()) return nullptr;
+  const at::Tensor *x, *ids;
+  if (!(x = take_logits(a[3], c, T, nullptr, "logits")) || !(ids = take_ids(a[4], c, T))) return nullptr;
+  const c10::cuda::CUDAGuard guard(c.ws->device());
+  at::Tensor logp, stats;
+  if (!c.out(logp, a[6], kF32, "float32", {T}, "token_logp") || !c.out(stats, a[7], kF32, "float32", {T, 2}, "row_stats"))
+    return nullptr;
+  const int rc = api.token_logp(c.plan, x->data_ptr(), dtype_of(*x), row_stride(*x), int32_t(x->size(1)),
+                                ids->data_ptr(), ids->scalar_type() == at::kLong, float(temperature),
+                                logp.data_ptr<float>(), stats.data_ptr<float>(), c.stream());
+  if (rc) return raise_code(rc, "pp_token_logp");
+  return Py_BuildValue("(NN)", THPVariable_Wrap(logp), THPVariable_Wrap(stats));
+  PP_GUARD_END
+}
+
+// token_logp_bwd(handle, workspace, T, logits, token_ids, token_logp, row_stats, d_token_logp, temperature,
+//                d_logits | None) -> d_logits
+PyObject* token_logp_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs(n, 10, "token_logp_bwd")) return nullptr;
+  PP_GUARD_BEGIN
+  Around c;
+  if (!c.begin(a[0], a[1])) return nullptr;
+  const int64_t T = PyLong_AsLongLong(a[2]);
+  const double temperature = PyFloat_AsDouble(a[8]);
+  if (PyErr_Occurred()) return nullptr;
+  const at::Tensor *x, *ids, *logp, *stats, *grad;
+  if (!(x = take_logits(a[3], c, T, nullptr, "logits")) || !(ids = take_ids(a[4], c, T)) ||
+      !(logp = c.take(a[5], kF32, "float32", {T}, "token_logp")) ||
+      !(stats = c.take(a[6], kF32, "float32", {T, 2}, "row_stats")) ||
+      !(grad = c.take(a[7], kF32, "float32", {T}, "d_token_logp")))
+    return nullptr;
+  const c10::cuda::CUDAGuard guard(c.ws->device());
+  at::Tensor out;
+  if (a[9] == Py_None) {
+    // (rows like those of the logits start alike to 16 bytes)
+    out = at::empty_strided({T, x->size(1)}, {row_stride(*x), 1}, x->options());
+  } else {
+    const at::Tensor* t = take_logits(a[9], c, T, x, "d_logits");
+    if (!t) return nullptr;
+    out = *t;
+  }
+  const int rc = api.token_logp_bwd(c.plan, x->data_ptr(), dtype_of(*x), row_stride(*x), int32_t(x->size(1)),
+                                    ids->data_ptr(), ids->scalar_type() == at::kLong, float(temperature),
+                                    logp->data_ptr<float>(), stats->data_ptr<float>(), grad->data_ptr<float>(),
+                                    out.data_ptr(), row_stride(out), c.stream());
+  if (rc) return raise_code(rc, "pp_token_logp_bwd");
+  return THPVariable_Wrap(out);
+  PP_GUARD_END
+}
+
+// policy_loss(handle, workspace, T, N, token_logp, old | None, ref | None, reward, mask | None, advantage mode,
+//             reduction, clip_low, clip_high, kl_coef, scale, eps, gradient wanted)
+//   -> (resp_loss, resp_kl, resp_clipped, advantage | None, d_token_logp | None)
+PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs(n, 17, "policy_loss")) return nullptr;
+  PP_GUARD_BEGIN
+  Around c;
+  if (!c.begin(a[0], a[1])) return nullptr;
+  const int64_t T = PyLong_AsLongLong(a[2]), N = PyLong_AsLongLong(a[3]);
+  pp_policy o;
+  o.advantage_mode = int32_t(PyLong_AsLong(a[9]));
+  o.reduction = int32_t(PyLong_AsLong(a[10]));
+  o.clip_low = PyFloat_AsDouble(a[11]);
+  o.clip_high = PyFloat_AsDouble(a[12]);
+  o.kl_coef = PyFloat_AsDouble(a[13]);
+  o.scale = PyFloat_AsDouble(a[14]);
+  o.eps = PyFloat_AsDouble(a[15]);
+  const int want = PyObject_IsTrue(a[16]);
+  if (PyErr_Occurred()) return nullptr;
+  const bool per_token = o.advantage_mode == PP_ADVANTAGE_TOKEN;
+  const at::Tensor *logp, *old = nullptr, *ref = nullptr, *reward, *mask = nullptr;
+  if (!(logp = c.take(a[4], kF32, "float32", {T}, "token_logp")) ||
+      (a[5] != Py_None && !(old = c.take(a[5], kF32, "float32", {T}, "old_token_logp"))) ||
+      (a[6] != Py_None && !(ref = c.take(a[6], kF32, "float32", {T}, "ref_token_logp"))) ||
+      !(reward = c.take(a[7], kF32, "float32", {per_token ? T : N}, "reward")) ||
+      (a[8] != Py_None && !(mask = c.take(a[8], at::kBool, "bool", {T}, "token_mask"))))
+    return nullptr;
+  const c10::cuda::CUDAGuard guard(c.ws->device());
+  // (one allocation for the numbers per response)
+  const int64_t row = (N + 3) / 4 * 4;
+  const at::Tensor per_resp = at::empty({per_token ? 3 : 4, row}, logp->options());
+  const at::Tensor grad = want ? at::empty({T}, logp->options()) : at::Tensor();
+  float* r = per_resp.data_ptr<float>();
+  auto f = [](const at::Tensor* t) { return t ? t->data_ptr<float>() : nullptr; };
+  const int rc = api.policy_loss(c.plan, &o, f(logp), f(old), f(ref), f(reward),
+                                 mask ? static_cast<const uint8_t*>(mask->data_ptr()) : nullptr,
+                                 per_token ? nullptr : r + 3 * row, r, r + row, r + 2 * row,
+                                 want ? grad.data_ptr<float>() : nullptr, c.stream());
+  if (rc) return raise_code(rc, "pp_policy_loss");
+  auto part = [&](int64_t i) { return THPVariable_Wrap(per_resp.select(0, i).narrow(0, 0, N)); };
+  auto none = [] { Py_INCREF(Py_None); return Py_None; };
+  return Py_BuildValue("(NNNNN)", part(0), part(1), part(2), per_token ? none() : part(3),
+                       want ? THPVariable_Wrap(grad) : none());
+  PP_GUARD_END
+}
+
 #define PP_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PP_METHOD(bind), PP_METHOD(build_plan), PP_METHOD(fwd), PP_METHOD(bwd),
-                         PP_METHOD(build_rows), PP_METHOD(assign_rows),
+                         PP_METHOD(build_rows), PP_METHOD(assign_rows), PP_METHOD(position_ids_axes),
+                         PP_METHOD(rope_qk_axes), PP_METHOD(token_logp), PP_METHOD(token_logp_bwd), PP_METHOD(policy_loss),
                          {nullptr, nullptr, 0, nullptr}};
 #define PP_STR2(x) #x
 #define PP_STR(x) PP_STR2(x)

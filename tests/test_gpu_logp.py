@@ -1,0 +1,317 @@
+"""GPU parity of the token log-probabilities and of the logits' gradient against the fp64 oracle.
+
+Tolerances (u = 2^-24, half a step of fp32).  l = log S, S a sum of V powers of two, each within 4 u from the function
+(2^-22) and u times its exponent's size from the argument's rounding; the part of a term with exponent -e is 2^-e / S, so that
+those errors add up to less than u (16 + 2 |l|).  A thread adds at most 512 terms one after the other (a row of 8 KB by one
+warp, or one of 256 KB by 512 threads in two sums) and the joins 16 more: u 528.  logp = (x_y - m) / temperature - l adds
+three roundings of its parts.  So |error| <= u (600 + 8 |l| + 8 |x_y - m| / temperature).
+The gradient's element g p: the exponent's argument, up to E = |m + l| log2(e) before K is taken off, comes from c x with c = log2(e)
+/ temperature rounded and m rounded once more: u (32 + 4 E) of itself, and l's own error above; then
+half a step of the logits' type, and of its smallest number."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import policy as P
+from paper_2602_24082_b200 import workloads as W
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+TYPES = {"bf16": (torch.bfloat16, 2.0 ** -8, 2.0 ** -126), "fp16": (torch.float16, 2.0 ** -11, 2.0 ** -25),
+         "fp32": (torch.float32, U, 2.0 ** -126)}
+
+STRUCTURES = {
+    "pair": [[(64, (32, 48))]],
+    "ragged": [[(57, (5, 28, 31))], [(1, (1, 30))]],
+    "ones": [[(1, (1,) * 37)], [(2, (1,))]],
+    "single": [[(9, (1,)), (1, (17,))]],
+    "one_token": [[(1, (1,))]],
+}
+
+
+def _plan(rows, **kw):
+    from paper_2602_24082_b200 import binding as B
+    return B.plan_for(W.Workload("logp", rows, 2, 1, 64, seed=0), **kw)
+
+
+def _inputs(rows, V, dtype, seed, stride=None, offset=0, ids_dtype=torch.int64):
+    T = sum(p + sum(rs) for row in rows for p, rs in row)
+    g = torch.Generator().manual_seed(seed)
+    x = 3 * torch.randn(T, V, generator=g)
+    ids = torch.randint(0, V, (T,), generator=g)
+    for r, t in P.predictions(rows):
+        if torch.rand((), generator=g) < 0.7:
+            x[r, ids[t]] += 12 * torch.rand((), generator=g)
+    stride = stride or V
+    buf = torch.full((T * stride + offset,), float("nan"), dtype=dtype, device="cuda")
+    view = buf[offset:].as_strided((T, V), (stride, 1))
+    view.copy_(x.to(dtype))
+    return view, ids.to(ids_dtype).cuda(), buf
+
+
+def _f64(t):
+    return t.double().cpu().numpy()
+
+
+def _check_fwd(rows, logits, ids, temperature, logp, stats):
+    x, y = _f64(logits), ids.cpu().numpy()
+    temp = float(np.float32(temperature))
+    want, st = P.token_logp(rows, x, y, temp)
+    logp, stats = _f64(logp), _f64(stats)
+    assert np.array_equal(np.isnan(logp), np.isnan(want))
+    l = np.zeros(len(want))
+    for r, t in P.predictions(rows):
+        l[t] = st[r, 1]
+    tol = U * (600 + 8 * np.abs(l) + 8 * np.abs(want + l))
+    fine = np.isfinite(want)
+    assert np.array_equal(logp[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)])
+    assert (np.abs(logp - want)[fine] <= tol[fine]).all(), np.abs(logp - want)[fine].max()
+    used = st.any(1)
+    assert not stats[~used].any()
+    assert (np.abs(stats - st)[:, 0] <= U * np.abs(st[:, 0])).all()
+    assert (np.abs(stats - st)[:, 1] <= U * (600 + 8 * np.abs(st[:, 1]))).all()
+
+
+def _check_bwd(rows, logits, ids, grad, temperature, d, kind):
+    _, half, tiny = TYPES[kind]
+    temp = float(np.float32(temperature))
+    x = _f64(logits)
+    want, size = P.token_logp_bwd(rows, x, ids.cpu().numpy(), _f64(grad), temp)
+    top = np.where(np.isfinite(x).any(1), np.where(np.isfinite(x), x, -np.inf).max(1), 0)
+    E = np.abs(top / temp) * 1.4427
+    E = np.where(E < 2.0 ** 19, E, 0) + np.log2(x.shape[1] + 1)      # (beyond, exp(x - m - l) itself is taken)
+    tol = half * np.abs(want) * (1 + 2 * half) + U * (700 + 8 * E)[:, None] * size + tiny
+    err = np.abs(_f64(d) - want)
+    assert (err <= tol).all(), (err / tol).max()
+
+
+VOCABS = [1, 2, 7, 8, 31, 257, 1000, 2048, 4099, 8200, 16391, 33000]
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("V", VOCABS)
+@pytest.mark.parametrize("structure", list(STRUCTURES))
+def test_parity(structure, V, kind):
+    from paper_2602_24082_b200 import binding as B
+    rows, seed = STRUCTURES[structure], V + len(structure)
+    layout = [dict(), dict(stride=V + 5), dict(offset=1), dict(stride=V + 8 - V % 8, ids_dtype=torch.int32)][seed % 4]
+    temperature = [1.0, 0.7][seed % 2]
+    logits, ids, buf = _inputs(rows, V, TYPES[kind][0], seed, **layout)
+    plan = _plan(rows, desc_on_device=seed % 3 == 0)
+    logp, stats = B.pp_token_logp(plan, logits, ids, temperature)
+    g = torch.randn(len(ids), generator=torch.Generator().manual_seed(seed)).cuda()
+    d = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g, temperature)
+    # ... into rows that lie otherwise than the logits', with room behind them
+    other = torch.full((len(ids), V + 3), 5.0, dtype=logits.dtype, device="cuda")
+    B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g, temperature, d_logits=other[:, :V])
+    torch.cuda.synchronize()
+    assert plan.status() == (0, 0)
+    assert d.stride(0) == logits.stride(0) or len(ids) == 1
+    _check_fwd(rows, logits, ids, temperature, logp, stats)
+    _check_bwd(rows, logits, ids, g, temperature, d, kind)
+    _check_bwd(rows, logits, ids, g, temperature, other[:, :V], kind)
+    assert (other[:, V:] == 5).all()
+    # in place, and what lies between the rows stays
+    before = buf.clone()
+    B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g, temperature, d_logits=logits)
+    assert torch.equal(logits, d)
+    logits.copy_(before[layout.get("offset", 0):].as_strided(logits.shape, logits.stride()))
+    assert torch.equal(buf.view(torch.uint8), before.view(torch.uint8))
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("V", [50257, 128256])
+@pytest.mark.parametrize("tokens", ["few", "more", "many"])
+def test_parity_of_large_vocabularies(tokens, V, kind):
+    """Rows that 8, 4, 2 and 1 blocks share, and those of 128 threads."""
+    from paper_2602_24082_b200 import binding as B
+    rows = {"few": [[(3, (2, 1))]], "more": [[(90, (20, 12))], [(60, (9,))]], "many": [[(700, (7, 5, 2))]]}[tokens]
+    logits, ids, _ = _inputs(rows, V, TYPES[kind][0], 3)
+    plan = _plan(rows)
+    g = torch.randn(len(ids), generator=torch.Generator().manual_seed(5)).cuda()
+    logp, stats = B.pp_token_logp(plan, logits, ids)
+    d = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g)
+    assert plan.status() == (0, 0)
+    used = sorted({r for r, _ in P.predictions(rows)})
+    assert not torch.cat([d[i:i + 1] for i in range(len(ids)) if i not in set(used)]).any()
+    _check_fwd(rows, logits, ids, 1.0, logp, stats)
+    _check_bwd(rows, logits, ids, g, 1.0, d, kind)
+
+
+@pytest.mark.parametrize("V,kind", [(100, "fp32"), (4099, "bf16"), (20000, "fp16"), (60000, "fp32"), (140000, "bf16")])
+def test_masked_and_extreme_logits(V, kind):
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(5, (6, 4, 3))], [(2, (9,))]]
+    dtype, lowest = TYPES[kind][0], torch.finfo(TYPES[kind][0]).min
+    logits, ids, _ = _inputs(rows, V, dtype, 1)
+    x = logits
+    x[:4] = float("nan")                       # rows that predict nothing are not read
+    x[10] = float("inf")                       # (the end of the first response)
+    x[4, V // 3:] = -float("inf")              # ids that cannot be sampled ...
+    ids[5] = V - 1                             # ... of which one was
+    x[5, :] = -float("inf")
+    x[5, V // 2] = -3.0                        # a single one left
+    ids[6] = V // 2
+    x[6] = lowest                              # nothing left: all alike
+    x[7] = lowest
+    x[7, 1] = 2.5
+    x[8] = -float("inf")                       # nothing at all
+    x[9, V - 1] = float("inf")
+    x[11, 0] = float("nan")
+    x[12] = lowest / 2
+    x[12, V - 2] = lowest / 4
+    ids[13] = V - 2
+    ids[16] = -1
+    ids[17] = V
+    plan = _plan(rows)
+    logp, stats = B.pp_token_logp(plan, logits, ids)
+    want, st = P.token_logp(rows, _f64(x), ids.cpu().numpy())
+    got = _f64(logp)
+    assert got[5] == -np.inf and abs(got[7] + np.log(V)) <= U * 700
+    # (certain tokens: 0 but for the bound above with l = 0 and x_y = m; fp16's lowest, -65504, is not far enough for exact terms)
+    assert abs(got[6]) <= U * 600 and abs(got[13]) <= U * 600
+    assert np.isnan(got[9:11]).all() and np.isnan(got[12]) and got[16] == 0 and np.isnan(got[17])
+    nan = np.isnan(want)
+    assert np.array_equal(np.isnan(got), nan)
+    fine = np.isfinite(want)
+    assert (np.abs(got - want)[fine] <= U * (600 + 8 * np.log(V) + 8 * np.abs(want[fine]))).all()
+    # gradients of the rows that are numbers
+    g = torch.randn(len(ids), generator=torch.Generator().manual_seed(5)).cuda()
+    g[torch.from_numpy(nan).cuda()] = 0
+    d = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g)
+    assert plan.status() == (0, 0)
+    safe = torch.where(torch.isnan(x) | (x == float("inf")), torch.zeros_like(x), x)
+    safe[8] = 0
+    _check_bwd(rows, safe, ids, g, 1.0, d, kind)
+
+
+@pytest.mark.parametrize("V", [50, 5000, 70000])
+def test_the_same_id_of_several_responses_and_gradients_that_cancel(V):
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(3, (2, 1, 4, 1, 1))], [(4, (1,) * 70)]]
+    logits, ids, _ = _inputs(rows, V, torch.float32, 2)
+    seqs = P.sequences(rows)
+    first = [y[0] for y in seqs[0][1]]
+    ids[first] = torch.tensor([7, 7, 9, -1, 7]).cuda()
+    ids[[y[0] for y in seqs[1][1]]] = torch.arange(70).cuda() % 3
+    g = torch.randn(len(ids), generator=torch.Generator().manual_seed(1)).cuda()
+    g[first] = torch.tensor([1.0, -3.0, 2.0, 9.0, 0.0]).cuda()      # those that count add up to zero
+    plan = _plan(rows)
+    logp, stats = B.pp_token_logp(plan, logits, ids)
+    d = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g)
+    _check_fwd(rows, logits, ids, 1.0, logp, stats)
+    _check_bwd(rows, logits, ids, g, 1.0, d, "fp32")
+
+
+def test_rows_without_a_gradient_are_not_read():
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(3, (4, 2))]]
+    logits, ids, _ = _inputs(rows, 3000, torch.bfloat16, 4)
+    plan = _plan(rows)
+    logp, stats = B.pp_token_logp(plan, logits, ids)
+    g = torch.zeros(len(ids), device="cuda")
+    g[4] = 1.0
+    logits[[0, 1, 2, 4, 5, 6, 7, 8]] = float("nan")
+    d = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g)
+    assert not d[[0, 1, 2, 4, 5, 6, 7, 8]].any() and d[3].float().abs().sum() > 0.1
+
+
+def test_gradient_against_differences():
+    """The log-probabilities of the kernel itself, moved by h in a direction: their sum's slope is the gradient's
+    product with it.  Differences of fp32 values of size 10: 2 u 600 / h, and h^2 for the curvature."""
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(3, (4, 2, 1))], [(5, (3,))]]
+    logits, ids, _ = _inputs(rows, 700, torch.float32, 6)
+    plan = _plan(rows)
+    g = torch.randn(len(ids), generator=torch.Generator().manual_seed(2)).cuda()
+    logp, stats = B.pp_token_logp(plan, logits, ids, 0.7)
+    d = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g, 0.7).double()
+    h = 2.0 ** -7
+    for seed in range(4):
+        v = torch.randn(logits.shape, generator=torch.Generator().manual_seed(seed)).cuda()
+        up, down = (B.pp_token_logp(plan, logits + s * h * v, ids, 0.7)[0].double() for s in (1, -1))
+        slope = ((up - down) * g.double()).sum() / (2 * h)
+        assert abs(float(slope - (d * v.double()).sum())) < float(g.abs().sum()) * (U * 700 / h + 8 * h * h)
+
+
+def test_offsets_beyond_32_bits():
+    """34000 rows of 131072 columns: elements beyond 2^32."""
+    from paper_2602_24082_b200 import binding as B
+    rows, V = [[(100, (4, 6))], [(33000, (400, 490))]], 131072
+    T = 34000
+    logits = torch.zeros(T, V, dtype=torch.bfloat16, device="cuda")
+    at = torch.arange(33105, T, 7, device="cuda")
+    at = torch.cat([torch.tensor([99, 101, 33109], device="cuda"), at])
+    logits[at] = torch.randn(len(at), V, generator=torch.Generator(device="cuda").manual_seed(0), device="cuda").bfloat16()
+    ids = (torch.arange(T, device="cuda") * 977) % V
+    plan = _plan(rows)
+    logp, stats = B.pp_token_logp(plan, logits, ids)
+    g = torch.ones(T, device="cuda")
+    d = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g, d_logits=logits)
+    assert d.data_ptr() == logits.data_ptr() and plan.status() == (0, 0)
+    for r, t in P.predictions(rows)[-60:]:
+        x = torch.zeros(V, dtype=torch.float64, device="cuda")
+        k = (at == r).nonzero()
+        if len(k):
+            x = torch.randn(len(at), V, generator=torch.Generator(device="cuda").manual_seed(0), device="cuda").bfloat16()[int(k[0])].double()
+        lp = torch.log_softmax(x, 0)
+        y = int(ids[t])
+        assert abs(float(logp[t] - lp[y])) < 2e-4
+        want = -lp.exp()
+        want[y] += 1
+        assert float((d[r].double() - want).abs().max()) < 2.0 ** -8
+
+
+@pytest.mark.parametrize("V", [300, 20000, 128256])
+def test_streams_graphs_and_repeats(V):
+    """The same bits every time: again, on another stream, and replayed from a graph on new inputs."""
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(40, (9, 20, 1))], [(3, (30,))]]
+    logits, ids, _ = _inputs(rows, V, torch.bfloat16, 8)
+    plan = _plan(rows)
+    g = torch.randn(len(ids), device="cuda")
+
+    def step():
+        logp, stats = B.pp_token_logp(plan, logits, ids)
+        return logp, stats, B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g)
+
+    want = step()
+    assert all(torch.equal(a, b) for a, b in zip(step(), want))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        there = step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            held = step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(there, want))
+    logits.copy_(torch.roll(logits, 1, 1))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(held, step()))
+    assert not torch.equal(held[0], want[0])
+
+
+def test_refusals():
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(3, (4, 2))]]
+    logits, ids, _ = _inputs(rows, 100, torch.bfloat16, 1)
+    plan = _plan(rows)
+    logp, stats = B.pp_token_logp(plan, logits, ids)
+    for bad in (logits[:-1], logits.double(), logits.T, logits.cpu(), logits[:, ::2], logits[0], logits[:, :0]):
+        with pytest.raises(ValueError):
+            B.pp_token_logp(plan, bad, ids)
+    for bad in (ids[:-1], ids.float(), ids.cpu(), ids[::2]):
+        with pytest.raises(ValueError):
+            B.pp_token_logp(plan, logits, bad)
+    for t in (0.0, -1.0, float("nan"), float("inf")):
+        with pytest.raises(B.PPError):
+            B.pp_token_logp(plan, logits, ids, t)
+    g = torch.ones(9, device="cuda")
+    for bad in (dict(d_logits=logits.float()), dict(d_logits=logits[:, :50]), dict(d_logits=logits[:5])):
+        with pytest.raises(ValueError):
+            B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g, **bad)
+    for args in ((logp[:-1], stats, g), (logp, stats.T, g), (logp, stats, g.double()), (logp, stats, g.cpu())):
+        with pytest.raises(ValueError):
+            B.pp_token_logp_bwd(plan, logits, ids, *args)

@@ -1,0 +1,149 @@
+"""One policy-training step of a layer on image prompts, all calls in a row as a program makes them, against fp64
+autograd on the unpacked sequences (x, y^k): positions with axes, rotary embedding out of a fused
+projection's buffer, packed attention, logits, log-probabilities, policy loss, and all the way back into the
+projection's gradient.
+
+Tolerance: between the projection's output and its gradient lie the roundings to bf16 of q and k, O, the logits, d logits, dO,
+P and dS inside the attention, dQ / dK / dV, and what is rotated back: eight on any path, each half a step, 2^-8 of its
+values (2-norm), which add up to 2^-5 at most."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import axes as A
+from oracle import policy as P
+from paper_2602_24082_b200 import workloads as W
+
+pytestmark = pytest.mark.gpu
+
+ROWS = [[(70, (40, 9, 130)), (21, (30, 1))], [(200, (64, 65, 17))]]
+STARTS, GRIDS = [3, 40, 274, 340], [(1, 5, 6), (2, 2, 3), (1, 3, 4), (1, 9, 11)]
+SECTIONS, BASE, V = (8, 12, 12), 10000.0, 517
+POLICY = dict(clip_low=0.2, clip_high=0.28, kl_coef=0.1, reduction="response", scale=0.125)
+
+
+def _reference(qkv, w, ids, old, ref, reward, Hq, Hkv, D):
+    """(total loss, d qkv) by autograd, sequence by sequence."""
+    leaf = qkv.double().cpu().requires_grad_()
+    wo, ids = w.double().cpu(), ids.cpu()
+    pos = torch.from_numpy(A.position_ids(ROWS, STARTS, GRIDS)).double()
+    axis = [a for a, n in enumerate(SECTIONS) for _ in range(n)]
+    freq = BASE ** (-2.0 * torch.arange(D // 2, dtype=torch.float64) / D)
+    adv = P.advantages(ROWS, reward.cpu(), "normalized")
+    total, logps, k = 0, torch.zeros(len(leaf), dtype=torch.float64), 0
+    for prompt, resp in P.sequences(ROWS):
+        for y in resp:
+            at = torch.tensor(list(prompt) + list(y))
+            x = leaf[at]
+            angle = (pos[axis][:, at].T * freq)[:, None]
+            c, s = angle.cos(), angle.sin()
+            turn = lambda z: torch.cat([z[..., :D // 2] * c - z[..., D // 2:] * s, z[..., D // 2:] * c + z[..., :D // 2] * s], -1)
+            q, key, v = turn(x[:, :Hq]), turn(x[:, Hq:Hq + Hkv]), x[:, Hq + Hkv:]
+            rep = lambda z: z.repeat_interleave(Hq // Hkv, 1)
+            score = torch.einsum("ihd,jhd->hij", q, rep(key)) * D ** -0.5
+            score = score.masked_fill(torch.ones(len(at), len(at)).triu(1).bool(), -torch.inf)
+            o = torch.einsum("hij,jhd->ihd", score.softmax(-1), rep(v)).flatten(1)
+            lp = torch.log_softmax(o[:-1] @ wo, -1)[torch.arange(len(at) - 1), ids[at[1:]]][len(prompt) - 1:]
+            logps[list(y)] = lp.detach()
+            if old is not None:
+                rho = (lp - old[list(y)]).exp()
+                d = ref[list(y)] - lp
+                total = total + POLICY["scale"] * (-torch.minimum(rho * adv[k], rho.clamp(0.8, 1.28) * adv[k])
+                                                   + 0.1 * (d.exp() - d - 1)).mean()
+            k += 1
+    if old is None:
+        return logps
+    total.backward()
+    return float(total.detach()), leaf.grad
+
+
+def test_step_matches_autograd_on_unpacked_sequences():
+    from paper_2602_24082_b200 import binding as B
+    Hq, Hkv, D = 4, 2, 64
+    w = W.Workload("step", ROWS, Hq, Hkv, D, seed=0)
+    T, N = w.total_tokens, 8
+    g = torch.Generator().manual_seed(0)
+    rand = lambda *shape: torch.randn(*shape, generator=g)
+    qkv = rand(T, Hq + 2 * Hkv, D).bfloat16().cuda()
+    wo = (rand(Hq * D, V) / 8).bfloat16().cuda()
+    ids = torch.randint(0, V, (T,), generator=g).cuda()
+    reward = rand(N).cuda()
+    # ratios of 1, 1.65 and 0.61, away from the borders at 0.8 and 1.28: rounded logits do not move a token across
+    lp = _reference(qkv, wo, ids, None, None, reward, Hq, Hkv, D)
+    old = (lp - 0.5 * torch.randint(-1, 2, (T,), generator=g)).float()
+    ref = (lp + 0.2 * rand(T)).float()
+    loss_want, d_want = _reference(qkv, wo, ids, old.double(), ref.double(), reward, Hq, Hkv, D)
+
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    plan = B.plan_for(w)
+    starts, grids, old, ref = i32(STARTS), i32(GRIDS), old.cuda(), ref.cuda()
+
+    def step():
+        pos, status = B.pp_position_ids_axes(plan, starts, grids)
+        q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:].contiguous()
+        new = lambda h: torch.empty(T, h, D, dtype=torch.bfloat16, device="cuda")
+        q, k = B.pp_rope_qk_axes(plan, q, k, pos, SECTIONS, BASE, q_out=new(Hq), k_out=new(Hkv))
+        o, lse = B.pp_attn_fwd(plan, q, k, v, D ** -0.5, for_backward=True)
+        logits = o.flatten(1) @ wo
+        logp, stats = B.pp_token_logp(plan, logits, ids)
+        loss, kl, clipped, adv, d_logp = B.pp_policy_loss(plan, logp, old, ref, reward, **POLICY)
+        d_logits = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, d_logp, d_logits=logits)
+        d_o = (d_logits @ wo.T).view(T, Hq, D)
+        dq, dk, dv = B.pp_attn_bwd(plan, q, k, v, o, lse, d_o, D ** -0.5)
+        d_qkv = torch.empty_like(qkv)
+        B.pp_rope_qk_axes(plan, dq, dk, pos, SECTIONS, BASE, inverse=True, q_out=d_qkv[:, :Hq], k_out=d_qkv[:, Hq:Hq + Hkv])
+        d_qkv[:, Hq + Hkv:] = dv
+        return loss, logp, d_qkv, status
+
+    loss, logp, d_qkv, status = step()
+    torch.cuda.synchronize()
+    assert plan.status() == (0, 0) and status.tolist() == [0, 0]
+    # (logits of size 2 in bf16: 2^-7 each way, and what O's rounding moves them by)
+    resp = [t for _, t in P.predictions(ROWS)]
+    assert float((logp.double().cpu() - lp)[resp].abs().max()) < 2.0 ** -4
+    assert abs(float(loss.double().sum()) - loss_want) < 2.0 ** -5 * (1 + abs(loss_want))
+    err = (d_qkv.double().cpu() - d_want).norm(dim=(0, 2)) / d_want.norm(dim=(0, 2))
+    assert float(err.max()) < 2.0 ** -5, err
+    # captured and replayed on other projections
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            held = step()
+    torch.cuda.synchronize()
+    qkv.copy_(qkv.flip(0))
+    graph.replay()
+    torch.cuda.synchronize()
+    again = step()
+    assert torch.equal(held[0], again[0]) and torch.equal(held[1], again[1]) and not torch.equal(held[1], logp)
+    assert float((held[2].double() - again[2].double()).norm() / again[2].double().norm()) < 2e-3   # (order of dQ's sums)
+
+
+def test_the_preference_loss_takes_the_same_log_probabilities():
+    """pp_token_logp -> pp_preference_loss -> pp_token_logp_bwd, against autograd on the logits."""
+    from paper_2602_24082_b200 import binding as B
+    w = W.Workload("dpo", ROWS, 4, 2, 64, seed=0)
+    T = w.total_tokens
+    g = torch.Generator().manual_seed(3)
+    logits = torch.randn(T, 300, generator=g).cuda()
+    ids = torch.randint(0, 300, (T,), generator=g, dtype=torch.int32).cuda()
+    plan = B.plan_for(w)
+    logp, stats = B.pp_token_logp(plan, logits, ids)
+    ref = logp + 0.1 * torch.randn(T, generator=g).cuda()
+    _, _, loss, d_logp = B.pp_preference_loss(plan, logp, ref, 0.1)
+    d = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, d_logp)
+    leaf = logits.double().requires_grad_()
+    r, t = (torch.tensor(x, device="cuda") for x in zip(*P.predictions(ROWS)))
+    lp = torch.log_softmax(leaf, -1)[r, ids.long()[t]]
+    at, total = 0, 0
+    full = torch.zeros(T, dtype=torch.float64, device="cuda").index_put((t,), lp - ref.double()[t])
+    for _, resp in P.sequences(ROWS):
+        reward = torch.stack([0.1 * full[y[0]:y[-1] + 1].sum() for y in resp])
+        pairs = [(a, b) for a in range(len(resp)) for b in range(a)]
+        total = total - sum(torch.nn.functional.logsigmoid(reward[a] - reward[b]) for a, b in pairs) / len(pairs)
+    total.backward()
+    # the loss is within 1e-4 (its own test), its gradient too; the logits' is a sum of products with it
+    assert abs(float(loss.double().sum() - total.detach())) < 1e-4 * float(total.detach())
+    assert float((d.double() - leaf.grad).norm() / leaf.grad.norm()) < 2e-4
