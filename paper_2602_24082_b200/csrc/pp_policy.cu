@@ -34,132 +34,161 @@ struct PolicyArgs {
 
 constexpr int kThreads = 256, kMaxParts = 8;
 
-// K sums over a team of kTeam threads of a block, or over all blocks of a cluster (which have started).
-template <int kTeam, int K>
-__device__ __forceinline__ void team_sum(double (&x)[K], double (*buf)[K], double (*slot)[K], int parts) {
+// What a team adds up.
+struct Sums {
+  double loss, kl;
+  int clipped, used;
+  __device__ __forceinline__ void add(const Sums& x) {
+    loss += x.loss;
+    kl += x.kl;
+    clipped += x.clipped;
+    used += x.used;
+  }
+};
+// ... over kTeam threads of a block, or over all blocks of a cluster (which have started).  (kCount: `used` alone)
+template <int kTeam, bool kCount>
+__device__ __forceinline__ Sums team_sum(Sums x, Sums* warp_of, Sums* part_of, int parts) {
+  x.used = __reduce_add_sync(0xffffffffu, x.used);
+  if constexpr (!kCount) {
+    x.clipped = __reduce_add_sync(0xffffffffu, x.clipped);
 #pragma unroll
-  for (int i = 0; i < K; ++i)
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
+    for (int o = 16; o > 0; o >>= 1) {
+      x.loss += __shfl_xor_sync(0xffffffffu, x.loss, o);
+      x.kl += __shfl_xor_sync(0xffffffffu, x.kl, o);
+    }
+  }
   if constexpr (kTeam > 32) {
     const int warp = threadIdx.x >> 5, first = warp / (kTeam / 32) * (kTeam / 32);
-    if ((threadIdx.x & 31) == 0)
-#pragma unroll
-      for (int i = 0; i < K; ++i) buf[warp][i] = x[i];
+    if ((threadIdx.x & 31) == 0) warp_of[warp] = x;
     if constexpr (kTeam == kThreads) __syncthreads();
     else named_barrier_sync(1 + threadIdx.x / kTeam, kTeam);
+    x = warp_of[first];
 #pragma unroll
-    for (int i = 0; i < K; ++i) {
-      x[i] = 0;
-      for (int w = 0; w < kTeam / 32; ++w) x[i] += buf[first + w][i];
-    }
+    for (int w = 1; w < kTeam / 32; ++w) x.add(warp_of[first + w]);
   }
   if constexpr (kTeam == kThreads) {
     if (parts > 1) {
       auto cluster = cooperative_groups::this_cluster();
-      if (threadIdx.x < parts)
-#pragma unroll
-        for (int i = 0; i < K; ++i) cluster.map_shared_rank(&slot[cluster.block_rank()][0], int(threadIdx.x))[i] = x[i];
+      if (threadIdx.x < parts) *cluster.map_shared_rank(part_of + cluster.block_rank(), int(threadIdx.x)) = x;
       cluster.sync();
-#pragma unroll
-      for (int i = 0; i < K; ++i) {
-        x[i] = 0;
-        for (int b = 0; b < parts; ++b) x[i] += slot[b][i];
-      }
+      x = part_of[0];
+      for (int b = 1; b < parts; ++b) x.add(part_of[b]);
     }
   }
+  return x;
 }
 
 template <int kTeam>
 __global__ void __launch_bounds__(kThreads) policy_loss_kernel(PolicyArgs p, int parts) {
-  __shared__ double buf[kThreads / 32][3], count_buf[kThreads / 32][1];
-  __shared__ double slot[kMaxParts][3], count_slot[kMaxParts][1];
+  __shared__ Sums warp_of[2][kThreads / 32], part_of[2][kMaxParts];
   dependency_wait();
-  if (p.header[0] != kStatusOk) return;
   const int lane = threadIdx.x & 31, in_team = threadIdx.x % kTeam;
   const int x = kTeam == kThreads ? blockIdx.x / parts : blockIdx.x * (kThreads / kTeam) + threadIdx.x / kTeam;
   const int part = kTeam == kThreads ? blockIdx.x % parts : 0;
   if (x >= p.N) return;
   if (kTeam == kThreads && parts > 1) cooperative_groups::this_cluster().barrier_arrive();
+  const int status = p.header[0];
   const int g = warp_upper(p.grp_resp_off, p.G, x);
-  const int x0 = p.grp_resp_off[g], n = p.grp_resp_off[g + 1] - x0;
-  const int sp = g + x0, seg = g + 1 + x;
+  const int seg = g + 1 + x;
   const int a = p.seg_start[seg], b = p.seg_start[seg + 1];
+  const int x0 = p.grp_resp_off[g], n = p.grp_resp_off[g + 1] - x0, sp = g + x0;
+  const int p0 = p.seg_start[sp], p1 = p.seg_start[sp + 1];
+  if (status != kStatusOk) return;
   const int stride = kTeam * parts, first = a + part * kTeam + in_team;
+  const bool per_token = p.o.advantage_mode == PP_ADVANTAGE_TOKEN;
+  // what a token needs; that of a thread's first is on its way while the advantage and the count are found
+  struct Token {
+    float lp, old, ref, adv;
+    bool use;
+  };
+  auto load = [&](int t) {
+    Token k{};
+    if (t < b) {
+      k.use = !p.mask || p.mask[t];
+      k.lp = p.logp[t];
+      if (p.old) k.old = p.old[t];
+      if (p.ref) k.ref = p.ref[t];
+      if (per_token) k.adv = p.reward[t];
+    }
+    return k;
+  };
+  Token k = load(first);
   if (p.d_logp) {   // this response's share of the prompt's zeros
-    const int p0 = p.seg_start[sp], len = p.seg_start[sp + 1] - p0, j = x - x0;
+    const int len = p1 - p0, j = x - x0;
     const int lo = p0 + int((long long)len * j / n), hi = p0 + int((long long)len * (j + 1) / n);
     for (int t = lo + part * kTeam + in_team; t < hi; t += stride) p.d_logp[t] = 0.f;
   }
   // the advantage, by every warp for itself
   double A = 0;
-  if (p.o.advantage_mode != PP_ADVANTAGE_TOKEN) {
+  if (!per_token) {
     A = p.reward[x];
     if (p.o.advantage_mode != PP_ADVANTAGE_GIVEN) {
-      double sum = 0;
-      for (int j = lane; j < n; j += 32) sum += p.reward[x0 + j];
+      const double inv_n = 1.0 / n, inv_n1 = n > 1 ? 1.0 / (n - 1) : 0.0;   // (under the loads)
+      const double mine = lane < n ? p.reward[x0 + lane] : 0.f;
+      double sum = mine;
+      for (int j = lane + 32; j < n; j += 32) sum += p.reward[x0 + j];
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      const double mean = sum / n;
+      const double mean = sum * inv_n;
       A -= mean;
       if (p.o.advantage_mode == PP_ADVANTAGE_NORMALIZED) {
-        double sq = 0;
-        for (int j = lane; j < n; j += 32) {
+        double sq = lane < n ? (mine - mean) * (mine - mean) : 0.0;
+        for (int j = lane + 32; j < n; j += 32) {
           const double d = p.reward[x0 + j] - mean;
           sq += d * d;
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-        A = n > 1 ? A / (sqrt(sq / (n - 1)) + p.o.eps) : 0.0;
+        A = n > 1 ? A / (sqrt(sq * inv_n1) + p.o.eps) : 0.0;
       }
     }
     if (p.advantage && part == 0 && in_team == 0) p.advantage[x] = float(A);
   }
   if (kTeam == kThreads && parts > 1) cooperative_groups::this_cluster().barrier_wait();
-  // tokens that count
-  double count = b - a;
-  if (p.mask) {
-    int c = 0;
+  // tokens that count: found first where the gradient has to be divided by their number
+  double w = p.o.scale;
+  if (p.o.reduction == PP_REDUCE_RESPONSE) {
+    double count = b - a;
+    if (p.mask) {
+      int c = k.use;
 #pragma unroll 4
-    for (int t = first; t < b; t += stride) c += p.mask[t] != 0;
-    double n_k[1] = {double(c)};
-    team_sum<kTeam>(n_k, count_buf, count_slot, parts);
-    count = n_k[0];
+      for (int t = first + stride; t < b; t += stride) c += p.mask[t] != 0;
+      count = team_sum<kTeam, true>(Sums{0, 0, 0, c}, warp_of[0], part_of[0], parts).used;
+    }
+    w = count > 0 ? p.o.scale / count : 0.0;
   }
-  const double inv = count > 0 ? 1.0 / count : 0.0;
-  const double w = p.o.reduction == PP_REDUCE_RESPONSE ? p.o.scale * inv : p.o.scale;
   const double low = 1.0 - p.o.clip_low, high = 1.0 + p.o.clip_high;
-  double loss = 0, kl = 0;
-  int clipped = 0;
-#pragma unroll 2
+  Sums sum{0, 0, 0, 0};
   for (int t = first; t < b; t += stride) {
+    const Token now = k;
+    k = load(t + stride);
     float d = 0.f;
-    if (!p.mask || p.mask[t]) {
-      const double lp = p.logp[t];
-      const double At = p.o.advantage_mode == PP_ADVANTAGE_TOKEN ? double(p.reward[t]) : A;
-      const double rho = p.old ? exp(lp - double(p.old[t])) : 1.0;
+    if (now.use) {
+      const double lp = now.lp, At = per_token ? double(now.adv) : A;
+      const double rho = p.old ? exp(lp - double(now.old)) : 1.0;
       // (comparisons, which keep a ratio that is no number)
       const double u = rho * At, v = (rho < low ? low : rho > high ? high : rho) * At;
       const bool cut = v < u;
       double term = cut ? -v : -u, slope = cut ? 0.0 : -u;
-      clipped += cut;
+      sum.clipped += cut;
+      ++sum.used;
       if (p.ref) {
-        const double delta = double(p.ref[t]) - lp, e = expm1(delta);
-        kl += e - delta;
+        const double delta = double(now.ref) - lp, e = expm1(delta);
+        sum.kl += e - delta;
         term += p.o.kl_coef * (e - delta);
         slope -= p.o.kl_coef * e;
       }
-      loss += term;
+      sum.loss += term;
       d = float(w * slope);
     }
     if (p.d_logp) p.d_logp[t] = d;
   }
-  double sum[3] = {loss, kl, double(clipped)};
-  team_sum<kTeam>(sum, buf, slot, parts);
+  sum = team_sum<kTeam, false>(sum, warp_of[1], part_of[1], parts);
   if (part == 0 && in_team == 0) {
-    p.loss[x] = float(w * sum[0]);
-    p.kl[x] = float(inv * sum[1]);
-    p.clipped[x] = float(inv * sum[2]);
+    const double inv = sum.used ? 1.0 / sum.used : 0.0;
+    p.loss[x] = float(w * sum.loss);
+    p.kl[x] = float(inv * sum.kl);
+    p.clipped[x] = float(inv * sum.clipped);
   }
 }
 
@@ -195,7 +224,7 @@ cudaError_t launch_policy_loss(const pp_plan* plan, const pp_policy& o, const fl
   if (mean <= 128) return launch_kernel(true, policy_loss_kernel<64>, dim3((N + 3) / 4), dim3(kThreads), 0, stream, p, 1);
   if (mean <= 256) return launch_kernel(true, policy_loss_kernel<128>, dim3((N + 1) / 2), dim3(kThreads), 0, stream, p, 1);
   int parts = 1;
-  while (parts < kMaxParts && mean > 512 * parts && (long long)N * 2 * parts <= 4ll * dev->num_sms) parts *= 2;
+  while (parts < kMaxParts && mean > kThreads * parts && (long long)N * 2 * parts <= 4ll * dev->num_sms) parts *= 2;
   return launch_clusters(parts, policy_loss_kernel<kThreads>, dim3(unsigned(N) * parts), dim3(kThreads), 0, stream, p,
                          parts);
 }
