@@ -15,6 +15,8 @@
 // others), bound by HBM; the inverse is the backward pass.
 #include <math.h>
 
+#include <algorithm>
+
 #include "pp_seg.cuh"
 
 namespace pp {
@@ -51,7 +53,17 @@ __device__ __forceinline__ int spans_before(const AxesArgs& p, int t) {
 
 constexpr int kPosThreads = 256, kPosChunk = 4 * kPosThreads;   // spans whose sums are at hand at a time
 
+// The array, copied to shared memory by the block if it has the room.
+template <int kRoom>
+__device__ __forceinline__ const int32_t* held(int32_t* to, const int32_t* from, int n) {
+  if (n > kRoom) return from;
+  for (int i = threadIdx.x; i < n; i += kPosThreads) to[i] = from[i];
+  return to;
+}
+
 __global__ void __launch_bounds__(kPosThreads) position_ids_axes_kernel(AxesArgs p) {
+  constexpr int kHeld = 1024;
+  __shared__ int32_t s_seg[kHeld], s_off[kHeld], s_span[kHeld];
   __shared__ uint32_t sums[kPosChunk];
   __shared__ uint32_t warp_sum[kPosThreads / 32];
   __shared__ int bad;
@@ -59,6 +71,11 @@ __global__ void __launch_bounds__(kPosThreads) position_ids_axes_kernel(AxesArgs
   dependency_wait();
   if (p.header[0] != kStatusOk) return;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  // the tables that are searched, at hand: a look-up in L2 takes as long as twenty here
+  p.seg_start = held<kHeld>(s_seg, p.seg_start, p.nseg + 1);
+  p.grp_resp_off = held<kHeld>(s_off, p.grp_resp_off, p.G + 1);
+  p.span_start = held<kHeld>(s_span, p.span_start, p.I);
+  __syncthreads();
   if (blockIdx.x == gridDim.x - 1) {   // one block looks the spans over
     if (tid == 0) bad = INT_MAX;
     __syncthreads();
@@ -199,41 +216,32 @@ struct RopeArgs {
 };
 
 // A thread takes eight frequencies -- 16 bytes of a head's lower half and 16 of its upper -- of every
-// `heads`-th head of a token, for which it computes sine and cosine once.
+// `heads`-th head of a token, four heads in all: as many as it has on their way at once.  The block computes each token's
+// sines and cosines once, in shared memory, under the first loads.  With more heads for a thread the batches follow each
+// other, with fewer too little is on its way: 65536 tokens, 40 heads, D 128 197 us with four, 228 with eight, 220
+// with two or three; 47325 tokens, 16 heads 62.5, 70 and 84; sines by every thread for its own eight frequencies
+// 203 and 63 at best, with ten and eight heads.
+constexpr int kRopeBatch = 4;
 template <int D>
 __host__ __device__ constexpr int rope_threads() { return D == 96 ? 192 : 256; }
 
 template <int D>
-__global__ void __launch_bounds__(rope_threads<D>())
+__global__ void __launch_bounds__(rope_threads<D>(), 3)
 rope_axes_kernel(RopeArgs p, const __grid_constant__ RopeTable table, int heads) {
-  constexpr int kChunks = D / 16, kHalf = D / 2;
-  __shared__ uint64_t s_turn[kHalf];
-  __shared__ uint8_t s_axis[kHalf];
-  if (threadIdx.x < kHalf) {
-    s_turn[threadIdx.x] = table.turn[threadIdx.x];
-    s_axis[threadIdx.x] = table.axis[threadIdx.x];
-  }
-  __syncthreads();
+  constexpr int kChunks = D / 16, kHalf = D / 2, kThreads = rope_threads<D>(), kSlots = kThreads / kChunks;
+  constexpr int kBatch = kRopeBatch;
+  // cosine and sine of two frequencies: [token][four pairs][chunk]
+  __shared__ float4 turned[kSlots * 4 * kChunks];
   dependency_wait();
   if (p.header[0] != kStatusOk) return;
-  const int chunk = threadIdx.x % kChunks, slot = threadIdx.x / kChunks;
-  const int per_block = rope_threads<D>() / kChunks / heads;
-  const long long t = (long long)blockIdx.x * per_block + slot / heads;
-  if (t >= p.T) return;
-  float c[8], s[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int f = chunk * 8 + i;
-    const long long at = p.pos[size_t(s_axis[f]) * p.T + t];
-    const uint64_t turn = uint64_t(at) * s_turn[f];
-    sincospif(float(int32_t(turn >> 32)) * 4.656612873077393e-10f, &s[i], &c[i]);   // (2^-31 half turns)
-    s[i] *= p.sign;
-  }
-  const int H = p.Hq + p.Hkv;
-  // (all loads of a few heads in front of their stores: the tensors may be the same)
-  constexpr int kBatch = 4;
-  for (int h0 = slot % heads; h0 < H; h0 += kBatch * heads) {
-    uint4 lo[kBatch], hi[kBatch];
+  const int per_block = kSlots / heads;
+  const long long t0 = (long long)blockIdx.x * per_block;
+  const int tokens = int(min((long long)per_block, p.T - t0));
+  const int chunk = threadIdx.x % kChunks, slot = threadIdx.x / kChunks, token = slot / heads, H = p.Hq + p.Hkv;
+  const long long t = t0 + token;
+  // a batch of heads is loaded in front of its stores (the tensors may be the same), the first under the sines
+  uint4 lo[kBatch], hi[kBatch];
+  auto load = [&](int h0) {
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
       const int h = h0 + j * heads;
@@ -243,6 +251,21 @@ rope_axes_kernel(RopeArgs p, const __grid_constant__ RopeTable table, int heads)
         hi[j] = reinterpret_cast<const uint4*>(src + kHalf)[chunk];
       }
     }
+  };
+  int h0 = token < tokens ? slot % heads : H;
+  load(h0);
+  for (int i = threadIdx.x; i < tokens * kHalf; i += kThreads) {
+    const int of = i / kHalf, f = i % kHalf;
+    const long long at = p.pos[size_t(table.axis[f]) * p.T + t0 + of];
+    const uint64_t turn = uint64_t(at) * table.turn[f];
+    float c, s;
+    sincospif(float(int32_t(turn >> 32)) * 4.656612873077393e-10f, &s, &c);   // (2^-31 half turns)
+    reinterpret_cast<float2*>(turned)[((of * 4 + f % 8 / 2) * kChunks + f / 8) * 2 + f % 2] = make_float2(c, s * p.sign);
+  }
+  __syncthreads();
+  if (token >= tokens) return;
+  const float4* mine = turned + token * 4 * kChunks + chunk;
+  for (; h0 < H; h0 += kBatch * heads) {
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
       const int h = h0 + j * heads;
@@ -251,25 +274,26 @@ rope_axes_kernel(RopeArgs p, const __grid_constant__ RopeTable table, int heads)
       uint32_t x[4], y[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
+        const float4 cs = mine[i * kChunks];   // cosine and sine of the pair's first, of its second
         const float a0 = __uint_as_float(l[i] << 16), a1 = __uint_as_float(l[i] & 0xffff0000u);
         const float b0 = __uint_as_float(u[i] << 16), b1 = __uint_as_float(u[i] & 0xffff0000u);
-        x[i] = pack_bf16(a0 * c[2 * i] - b0 * s[2 * i], a1 * c[2 * i + 1] - b1 * s[2 * i + 1]);
-        y[i] = pack_bf16(b0 * c[2 * i] + a0 * s[2 * i], b1 * c[2 * i + 1] + a1 * s[2 * i + 1]);
+        x[i] = pack_bf16(a0 * cs.x - b0 * cs.y, a1 * cs.z - b1 * cs.w);
+        y[i] = pack_bf16(b0 * cs.x + a0 * cs.y, b1 * cs.z + a1 * cs.w);
       }
       __nv_bfloat16* dst =
           h < p.Hq ? p.q_out + t * p.q_out_stride + h * D : p.k_out + t * p.k_out_stride + (h - p.Hq) * D;
       reinterpret_cast<uint4*>(dst)[chunk] = make_uint4(x[0], x[1], x[2], x[3]);
       reinterpret_cast<uint4*>(dst + kHalf)[chunk] = make_uint4(y[0], y[1], y[2], y[3]);
     }
+    load(h0 + kBatch * heads);
   }
 }
 
 template <int D>
-cudaError_t launch_rope_of(const RopeArgs& p, const RopeTable& table, int num_sms, cudaStream_t stream) {
+cudaError_t launch_rope_of(const RopeArgs& p, const RopeTable& table, cudaStream_t stream) {
   constexpr int kSlots = rope_threads<D>() / (D / 16);
   const int H = p.Hq + p.Hkv;
-  int heads = 1;
-  while (heads < kSlots && heads < H && (heads * 8 < H || (long long)p.T * heads < 8ll * kSlots * num_sms)) heads *= 2;
+  const int heads = std::min(kSlots, (H + kRopeBatch - 1) / kRopeBatch);
   const int per_block = kSlots / heads;
   return launch_kernel(true, rope_axes_kernel<D>, dim3(unsigned((p.T + (long long)per_block - 1) / per_block)),
                        dim3(rope_threads<D>()), 0, stream, p, table, heads);
@@ -299,15 +323,13 @@ cudaError_t launch_rope_axes(const pp_plan* plan, const void* q, long long q_str
                              void* q_out, long long q_out_stride, void* k_out, long long k_out_stride,
                              const int32_t* pos, const uint8_t* axis_of_freq, float base, bool inverse,
                              cudaStream_t stream) {
-  static DeviceSetup setup[kMaxDevices];
-  const DeviceSetup* dev = device_setup(setup);
-  if (!dev) return cudaErrorInvalidDevice;
   const int D = plan->prob.head_dim;
+  // base^(-2i/D) / (2 pi) turns per position, below 0.16: one power, and products with 64 bits
   RopeTable table = {};
-  for (int i = 0; i < D / 2; ++i) {
-    // base^(-2i/D) / (2 pi) turns per position, below 0.16
-    const double turns = pow(double(base), -2.0 * i / D) / 6.283185307179586477;
-    table.turn[i] = uint64_t(ldexp(turns, 64));
+  const long double ratio = powl((long double)base, -2.0L / D);
+  long double turns = 0.159154943091895335768883763372514362L;
+  for (int i = 0; i < D / 2; ++i, turns *= ratio) {
+    table.turn[i] = uint64_t(ldexpl(turns, 64));
     table.axis[i] = axis_of_freq[i];
   }
   RopeArgs p;
@@ -325,9 +347,9 @@ cudaError_t launch_rope_axes(const pp_plan* plan, const void* q, long long q_str
   p.k_out_stride = k_out_stride;
   p.pos = pos;
   p.sign = inverse ? -1.f : 1.f;
-  return D == 128  ? launch_rope_of<128>(p, table, dev->num_sms, stream)
-         : D == 96 ? launch_rope_of<96>(p, table, dev->num_sms, stream)
-                   : launch_rope_of<64>(p, table, dev->num_sms, stream);
+  return D == 128  ? launch_rope_of<128>(p, table, stream)
+         : D == 96 ? launch_rope_of<96>(p, table, stream)
+                   : launch_rope_of<64>(p, table, stream);
 }
 
 }  // namespace pp
