@@ -49,8 +49,8 @@ int check_problem_shape(const pp_problem* p) {
   return PP_OK;
 }
 
-// Complete validation of host-side descriptors.
-int check_host_descriptors(const pp_problem* p) {
+// Complete validation of host-side descriptors.  *resp_tokens: what the responses hold.
+int check_host_descriptors(const pp_problem* p, long long* resp_tokens = nullptr) {
   if (!p->row_group_off || !p->grp_prompt_len || !p->grp_resp_off || !p->resp_len)
     return PP_ERR_INVALID_ARG;
   if (p->row_group_off[0] != 0 || p->row_group_off[p->num_rows] != p->num_groups)
@@ -65,11 +65,13 @@ int check_host_descriptors(const pp_problem* p) {
     if (p->grp_resp_off[g + 1] <= p->grp_resp_off[g]) return PP_ERR_INVALID_ARG;
     total += p->grp_prompt_len[g];
   }
+  const long long prompts = total;
   for (int x = 0; x < p->num_responses; ++x) {
     if (p->resp_len[x] < 1) return PP_ERR_INVALID_ARG;
     total += p->resp_len[x];
   }
   if (total != p->total_tokens) return PP_ERR_INVALID_ARG;
+  if (resp_tokens) *resp_tokens = total - prompts;
   return PP_OK;
 }
 
@@ -102,8 +104,9 @@ static int build_plan(const pp_problem* problem, const pp_problem* whole, void* 
     return PP_ERR_INVALID_ARG;
   pp::PlanLayout lay = pp::plan_layout(*problem);
   if (workspace_bytes < lay.total) return PP_ERR_WORKSPACE_TOO_SMALL;
+  long long resp_tokens = 0;
   if (!problem->desc_on_device) {
-    rc = check_host_descriptors(problem);
+    rc = check_host_descriptors(problem, &resp_tokens);
     if (rc) return rc;
   }
   // first call that touches a device: everything above is host-side validation
@@ -112,6 +115,7 @@ static int build_plan(const pp_problem* problem, const pp_problem* whole, void* 
   pp_plan* plan = new (std::nothrow) pp_plan;
   if (!plan) return PP_ERR_CUDA;
   plan->prob = *problem;
+  plan->resp_tokens = resp_tokens;
   plan->nseg = problem->num_groups + problem->num_responses;
   plan->max_tiles = pp::max_tiles_of(*problem);
   plan->ws = static_cast<char*>(d_workspace);

@@ -118,6 +118,7 @@ struct pp_plan {
   bool mixed;     // the forward runs over mixed query tiles (fwd_mixed_tiles)
   bool paired;    // ... takes tiles of a segment by twos (fwd_paired_tiles)
   int lg_split;   // log2 of the parts each backward unit is cut into (bwd_split_log2)
+  long long resp_tokens = 0;   // tokens of all responses, 0 where only the device knows
   // backward scratch whose dQ accumulator the latest forward on this plan has cleared
   mutable const void* cleared_scratch = nullptr;
 };

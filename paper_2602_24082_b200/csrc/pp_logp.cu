@@ -24,12 +24,15 @@
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 #include "pp_seg.cuh"
 
 namespace pp {
 namespace {
 
-constexpr float kFar = 524288.f;   // |c m| up to which K is a whole number apart from c m by less than 1.1
+constexpr float kFar = 524288.f;   // |c m| up to which ceil(c m) is at most 1 above c m
+constexpr int kMostK = 1 << 20;
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr double kLog2e = 1.4426950408889634074;
 
@@ -50,6 +53,7 @@ struct LogpArgs {
 template <typename X> struct Row;
 template <> struct Row<__nv_bfloat16> {
   static constexpr int kN = 8;
+  static constexpr uint32_t kLeast = 0xff80ff80u;   // -inf, twice
   static __device__ __forceinline__ float one(const __nv_bfloat16& x) { return __bfloat162float(x); }
   static __device__ __forceinline__ void store(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
   static __device__ __forceinline__ void pair(uint32_t w, float& a, float& b) {
@@ -69,6 +73,7 @@ template <> struct Row<__nv_bfloat16> {
 };
 template <> struct Row<__half> {
   static constexpr int kN = 8;
+  static constexpr uint32_t kLeast = 0xfc00fc00u;
   static __device__ __forceinline__ float one(const __half& x) { return __half2float(x); }
   static __device__ __forceinline__ void store(__half* p, float x) { *p = __float2half_rn(x); }
   static __device__ __forceinline__ void pair(uint32_t w, float& a, float& b) {
@@ -92,6 +97,7 @@ template <> struct Row<__half> {
 };
 template <> struct Row<float> {
   static constexpr int kN = 4;
+  static constexpr uint32_t kLeast = 0xff800000u;
   static __device__ __forceinline__ float one(const float& x) { return x; }
   static __device__ __forceinline__ void store(float* p, float x) { *p = x; }
   static __device__ __forceinline__ uint32_t max_word(uint32_t a, uint32_t b) {
@@ -127,222 +133,276 @@ __device__ __forceinline__ uint4 load_row(const void* p) {
 
 // ---------------------------------------------------------------- what a row predicts
 struct Predicts {
-  int n;       // tokens; 0 = nothing
-  int token;   // n == 1: the token.  Otherwise the responses' first tokens: starts of segments
-  int seg;     //   seg + 1 .. seg + n
+  int r;         // the row
+  int n;         // tokens; 0 = nothing
+  int seg;       // n == 1: token r + 1.  Otherwise the responses' first tokens: starts of segments seg + 1 .. seg + n
+  int id;        // n == 1: the token's id, -1 for any negative one and INT_MAX for any beyond
   bool prompt;
 };
-// (by a whole warp)
-__device__ __forceinline__ Predicts predicts_of(const LogpArgs& p, int r) {
+__device__ __forceinline__ int id_of(const LogpArgs& p, int t) {
+  if (!p.ids_64) return static_cast<const int32_t*>(p.ids)[t];
+  const long long y = static_cast<const long long*>(p.ids)[t];
+  return y < 0 ? -1 : y > INT_MAX ? INT_MAX : int(y);
+}
+// (By a whole warp.  The loads are few and mostly side by side: in small calls, and for short rows, this chain is what
+// counts.  A plan that was refused leaves searches that end, on whatever its tables hold.)
+__device__ __forceinline__ Predicts predicts_of(const LogpArgs& p, int r, bool& fine) {
+  const int status = p.header[0], seen = p.key_end[r];   // seen: where the keys of a prompt's tokens, or of a response's, end
   Predicts u;
+  u.r = r;
+  u.id = id_of(p, min(r + 1, p.T - 1));
   u.seg = warp_upper(p.seg_start, p.nseg, r);
-  const int a = p.seg_start[u.seg], e = p.seg_start[u.seg + 1];
-  const int seen = p.key_end[a];       // behind the group for a prompt's keys, behind the response for its own
-  u.prompt = seen > e;
+  // where the next segments start: this one's end, and perhaps the group's
+  const int start = p.seg_start[min(u.seg + 1 + int(threadIdx.x & 31), p.nseg)];
+  const int e = __shfl_sync(0xffffffffu, start, 0);
+  fine = status == kStatusOk;
+  u.prompt = seen > e;   // (behind the group)
   u.n = 0;
-  u.token = r + 1;
-  if (!u.prompt) u.n = r + 1 < e;
-  else if (r + 1 == e) u.n = warp_upper(p.seg_start, p.nseg, seen - 1) - u.seg;
+  if (!fine) return u;
+  if (!u.prompt) {
+    u.n = r + 1 < e;
+  } else if (r + 1 == e) {   // as many as there are segments up to the group's end
+    const unsigned at = __ballot_sync(0xffffffffu, start == seen);
+    u.n = at ? __ffs(at) - 1 : warp_upper(p.seg_start, p.nseg, seen - 1) - u.seg;
+  }
   return u;
 }
 __device__ __forceinline__ int token_of(const LogpArgs& p, const Predicts& u, int k) {
-  return u.n == 1 ? u.token : p.seg_start[u.seg + 1 + k];
-}
-__device__ __forceinline__ long long id_of(const LogpArgs& p, int t) {
-  return p.ids_64 ? static_cast<const long long*>(p.ids)[t] : (long long)static_cast<const int32_t*>(p.ids)[t];
+  return u.n == 1 ? u.r + 1 : p.seg_start[u.seg + 1 + k];
 }
 
-// The part of a row that `parts` blocks share: vectors [v0, v1) from the first 16-byte boundary on; the
-// elements before it (head) and behind the last whole vector (tail) go to the first block and the last.
+// The part of a row that 2^lg_parts blocks share: vectors [v0, v1) from the first boundary of kAlign bytes on; the
+// `edge` elements before it and the `tail` ones behind the last whole vector go to the first block and the last.
 struct Span {
   int head, v0, v1, tail0;   // elements in front; vectors; first element behind the vectors
+  int edge, tail;
 };
-template <typename X>
-__device__ __forceinline__ Span span_of(const X* row, int V, int part, int parts) {
+template <int kAlign, typename X>
+__device__ __forceinline__ Span span_of(const X* row, int V, int part, int lg_parts) {
   constexpr int kN = Row<X>::kN;
   Span s;
-  s.head = min(V, int(((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / sizeof(X)));
-  const int nv = (V - s.head) / kN, per = (nv + parts - 1) / parts;
+  s.head = min(V, int(((kAlign - (reinterpret_cast<uintptr_t>(row) & (kAlign - 1))) & (kAlign - 1)) / sizeof(X)));
+  const int nv = (V - s.head) / kN, per = (nv + (1 << lg_parts) - 1) >> lg_parts;
   s.v0 = min(nv, part * per);
   s.v1 = min(nv, s.v0 + per);
   s.tail0 = s.head + nv * kN;
+  s.edge = part == 0 ? s.head : 0;
+  s.tail = part + 1 == 1 << lg_parts ? V - s.tail0 : 0;
   return s;
 }
 
-// Running maximum and sum of 2^(c x - K), K a whole number (or -inf before anything finite).
+// Running maximum and sum of 2^(c x - K), K a whole number.
 struct Running {
-  float m = -INFINITY, K = -INFINITY, s = 0.f;
+  float m = -INFINITY, s = 0.f;
+  int K = -kMostK;
 };
-__device__ __forceinline__ float rescale(float from, float to) {   // 2^(from - to), from <= to
-  return from == to ? 1.f : exp2f(from - to);
+// K of a maximum m; where that is beyond +-2^20, the row goes through the second pass anyway
+__device__ __forceinline__ int whole(float cm) { return int(fminf(fmaxf(ceilf(cm), float(-kMostK)), float(kMostK))); }
+__device__ __forceinline__ float power(int from, int to) {   // 2^(from - to), from <= to: exact, and 0 far below
+  return __int_as_float(max(127 + from - to, 0) << 23);
 }
-__device__ __forceinline__ void join(Running& a, float m, float K, float s) {
-  a.m = fmaxf(a.m, m);
-  const float top = fmaxf(a.K, K);
-  a.s = a.s * rescale(a.K, top) + s * rescale(K, top);
-  a.K = top;
+// floats in the order of signed whole numbers, and back
+__device__ __forceinline__ int ordered(float x) {
+  const int i = __float_as_int(x);
+  return i ^ ((i >> 31) & 0x7fffffff);
 }
+__device__ __forceinline__ float from_ordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
 template <int kWarps>
 __device__ __forceinline__ void row_sync() {
   if constexpr (kWarps == 1) __syncwarp(); else __syncthreads();
 }
-
-// All threads of the row get the whole row's values.
-template <int kWarps>
-__device__ __forceinline__ Running join_row(Running a, float (*part_of)[4], float (*warp_of)[4], int parts, bool first) {
+// over the first kLanes lanes of a warp; all get the result
+template <int kLanes>
+__device__ __forceinline__ Running join_lanes(Running a) {
+  const int K = __reduce_max_sync(0xffffffffu, a.K);
+  a.s *= power(a.K, K);
+  a.K = K;
+  a.m = from_ordered(__reduce_max_sync(0xffffffffu, ordered(a.m)));
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
-    join(a, __shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.K, o),
-         __shfl_xor_sync(0xffffffffu, a.s, o));
-  if constexpr (kWarps > 1) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (lane == 0) {
-      warp_of[warp][0] = a.m;
-      warp_of[warp][1] = a.K;
-      warp_of[warp][2] = a.s;
-    }
-    __syncthreads();
-    a = Running();
-    if (lane < kWarps) {
-      a.m = warp_of[lane][0];
-      a.K = warp_of[lane][1];
-      a.s = warp_of[lane][2];
-    }
-#pragma unroll
-    for (int o = kWarps / 2; o > 0; o >>= 1)
-      join(a, __shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.K, o),
-           __shfl_xor_sync(0xffffffffu, a.s, o));
-    if (parts > 1) {
-      auto cluster = cooperative_groups::this_cluster();
-      if (first) cluster.barrier_wait();   // (all blocks have started: their arrival is before the row's loads)
-      const int me = int(cluster.block_rank());
-      if (warp == 0 && lane < 3) {
-        const float v = lane == 0 ? a.m : lane == 1 ? a.K : a.s;
-        for (int b = 0; b < parts; ++b) cluster.map_shared_rank(&part_of[me][0], b)[lane] = v;
-      }
-      cluster.sync();
-      a = Running();
-      for (int b = 0; b < parts; ++b) join(a, part_of[b][0], part_of[b][1], part_of[b][2]);
-    }
-  }
-  // (every thread of the last lanes may hold nothing: all take what lane 0 has)
-  a.m = __shfl_sync(0xffffffffu, a.m, 0);
-  a.K = __shfl_sync(0xffffffffu, a.K, 0);
-  a.s = __shfl_sync(0xffffffffu, a.s, 0);
+  for (int o = kLanes / 2; o > 0; o >>= 1) a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
   return a;
 }
 
-constexpr int kMaxParts = 8;
-template <int kWarps> constexpr int block_threads() { return kWarps == 1 ? 256 : kWarps * 32; }
-
-template <typename X, int kWarps>
-__global__ void __launch_bounds__(block_threads<kWarps>())
-token_logp_kernel(LogpArgs p, int parts, float* logp, float2* stats) {
-  constexpr int kN = Row<X>::kN, kThreads = kWarps * 32, kUnroll = 4;
-  __shared__ float warp_of[2][kWarps][4];
-  __shared__ float part_of[2][kMaxParts][4];
-  dependency_wait();
-  if (p.header[0] != kStatusOk) return;
-  const int tid = kWarps == 1 ? threadIdx.x & 31 : threadIdx.x;
-  const int r = kWarps == 1 ? blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x / parts;
-  const int part = kWarps == 1 ? 0 : blockIdx.x % parts;
-  if (r >= p.T) return;
-  const Predicts u = predicts_of(p, r);
-  const bool writes = part == 0;
-  if (u.prompt && writes && tid == 0) logp[r] = 0.f;
-  bool any = false;
-  for (int k = tid & 31; k < u.n; k += 32) any |= id_of(p, token_of(p, u, k)) >= 0;
-  if (!__any_sync(0xffffffffu, any)) {
-    if (writes) {
-      if (tid == 0) stats[r] = make_float2(0.f, 0.f);
-      for (int k = tid; k < u.n; k += kThreads) logp[token_of(p, u, k)] = 0.f;
+struct JoinSpace {
+  Running warp[8], part[8];
+};
+// All threads of the row get the whole row's values.
+template <int kWarps>
+__device__ __forceinline__ Running join_row(Running a, JoinSpace* space, int parts, bool first) {
+  a = join_lanes<32>(a);
+  if constexpr (kWarps > 1) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (lane == 0) space->warp[warp] = a;
+    __syncthreads();
+    a = lane < kWarps ? space->warp[lane] : Running();
+    a = join_lanes<32>(a);
+    if (parts > 1) {
+      auto cluster = cooperative_groups::this_cluster();
+      if (first) cluster.barrier_wait();   // (all blocks have started: their arrival is before the row's loads)
+      if (warp == 0 && lane < parts) *cluster.map_shared_rank(&space->part[cluster.block_rank()], lane) = a;
+      cluster.sync();
+      a = lane < parts ? space->part[lane] : Running();
+      a = join_lanes<32>(a);
     }
-    return;
   }
-  if constexpr (kWarps > 1)
-    if (parts > 1) cooperative_groups::this_cluster().barrier_arrive();
-  const X* row = static_cast<const X*>(p.logits) + (long long)r * p.row_stride;
-  const Span sp = span_of(row, p.V, part, parts);
+  return a;
+}
+
+constexpr int kMaxLgParts = 3;
+template <int kWarps> constexpr int block_threads() { return kWarps == 1 ? 128 : kWarps * 32; }
+template <int kWarps, int kUnroll> constexpr int blocks_per_sm() { return kWarps > 1 ? 32 / kWarps : kUnroll > 2 ? 8 : 12; }
+// A row's team: a warp (four to a block), a block, or a cluster of 2^lg_parts blocks.
+template <int kWarps> __device__ __forceinline__ int team_of(int lg_parts) {
+  return kWarps == 1 ? blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x >> lg_parts;
+}
+
+// Whether one of a row's tokens counts; the log-probabilities and statistics of a row that is not read.
+__device__ __forceinline__ bool row_used(const LogpArgs& p, const Predicts& u, bool writes, float* logp, float2* stats) {
+  const int lane = threadIdx.x & 31;
+  if (u.prompt && writes && lane == 0) logp[u.r] = 0.f;
+  bool any = u.n == 1 && u.id >= 0;
+  if (u.n > 1) {
+    for (int k = lane; k < u.n; k += 32) any |= id_of(p, token_of(p, u, k)) >= 0;
+    any = __any_sync(0xffffffffu, any);
+  }
+  if (!any && writes) {
+    if (lane == 0) stats[u.r] = make_float2(0.f, 0.f);
+    for (int k = lane; k < u.n; k += 32) logp[token_of(p, u, k)] = 0.f;
+  }
+  return any;
+}
+
+template <typename X, int kWarps, int kUnroll>
+__device__ __forceinline__ void token_logp_row(const LogpArgs& p, const Predicts& u, int part, int lg_parts,
+                                               JoinSpace* space, float* logp, float2* stats) {
+  constexpr int kN = Row<X>::kN, kThreads = kWarps * 32, kStep = kUnroll * kThreads;
+  const int tid = kWarps == 1 ? threadIdx.x & 31 : threadIdx.x;
+  const X* row = static_cast<const X*>(p.logits) + (long long)u.r * p.row_stride;
+  const Span sp = span_of<16>(row, p.V, part, lg_parts);
   const uint4* vec = reinterpret_cast<const uint4*>(row + sp.head);
   const float c = p.c;
   const uint64_t c2 = pack2(c, c);
-
+  uint4 va[kUnroll], vb[kUnroll];
+  auto load = [&](uint4 (&v)[kUnroll], int at) {
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) {
+      v[i] = make_uint4(Row<X>::kLeast, Row<X>::kLeast, Row<X>::kLeast, Row<X>::kLeast);
+      if (at + i * kThreads < sp.v1) v[i] = load_row(vec + at + i * kThreads);
+    }
+  };
+  load(va, sp.v0 + tid);
+  // the first tokens' own logits
+  float own = 0.f;
+  if (part == 0 && tid < u.n) {
+    const int y = u.n == 1 ? u.id : id_of(p, token_of(p, u, tid));
+    if (y >= 0 && y < p.V) own = Row<X>::one(row[y]);
+  }
   Running run;
   uint64_t sum = pack2(0.f, 0.f);
   auto raise = [&](float bm) {
-    const float K = ceilf(bm * c);
+    const int K = whole(bm * c);
     run.m = fmaxf(run.m, bm);
     if (K > run.K) {
-      const float f = exp2f(run.K - K);
+      const float f = power(run.K, K);
       sum = mul2(sum, pack2(f, f));
       run.K = K;
     }
-    return run.K == -INFINITY ? 0.f : -run.K;
+    return -float(run.K);
   };
-  // elements in front of the first boundary and behind the last, one per thread
-  {
-    const int edge = (part == 0 ? sp.head : 0), tail = part == parts - 1 ? p.V - sp.tail0 : 0;
-    for (int i = tid; i < edge + tail; i += kThreads) {
-      const float x = Row<X>::one(row[i < edge ? i : sp.tail0 + i - edge]);
-      const float k = raise(x);
-      sum = add2(sum, pack2(ex2(fmaf(x, c, k)), 0.f));
-    }
-  }
-  auto take = [&](const uint4* v, int n) {
+  auto take = [&](const uint4 (&v)[kUnroll], int n) {   // (n: vectors that some thread has)
     uint32_t w = Row<X>::max_word(Row<X>::max_word(v[0].x, v[0].y), Row<X>::max_word(v[0].z, v[0].w));
 #pragma unroll
     for (int i = 1; i < kUnroll; ++i)
-      if (i < n)
+      if (kWarps > 1 || i < n)
         w = Row<X>::max_word(w, Row<X>::max_word(Row<X>::max_word(v[i].x, v[i].y), Row<X>::max_word(v[i].z, v[i].w)));
     const float k = raise(Row<X>::max_of(w));
     const uint64_t k2 = pack2(k, k);
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i)
-      if (i < n)
+      if (kWarps > 1 || i < n)
         for_pairs<X>(v[i], [&](float a, float b) {
           float y, z;
           unpack2(fma2(pack2(a, b), c2, k2), y, z);
           sum = add2(sum, pack2(ex2(y), ex2(z)));
         });
   };
-  int at = sp.v0 + tid;
-  uint4 v[kUnroll];
-  for (; at + (kUnroll - 1) * kThreads < sp.v1; at += kUnroll * kThreads) {
-#pragma unroll
-    for (int i = 0; i < kUnroll; ++i) v[i] = load_row(vec + at + i * kThreads);
-    take(v, kUnroll);
+  // elements in front of the first boundary and behind the last, one per thread
+  for (int i = tid; i < sp.edge + sp.tail; i += kThreads) {
+    const float x = Row<X>::one(row[i < sp.edge ? i : sp.tail0 + i - sp.edge]);
+    const float k = raise(x);
+    sum = add2(sum, pack2(ex2(fmaf(x, c, k)), 0.f));
   }
-  for (; at < sp.v1; at += kThreads) {
-    v[0] = load_row(vec + at);
-    take(v, 1);
+  // one batch of vectors is on its way while the one before it is summed up
+  for (int at = sp.v0; at < sp.v1; at += 2 * kStep) {
+    load(vb, at + tid + kStep);
+    take(va, (sp.v1 - at + kThreads - 1) / kThreads);
+    load(va, at + tid + 2 * kStep);
+    if (at + kStep < sp.v1) take(vb, (sp.v1 - at - kStep + kThreads - 1) / kThreads);
   }
   float lo, hi;
   unpack2(sum, lo, hi);
   run.s = lo + hi;
-  run = join_row<kWarps>(run, part_of[0], warp_of[0], parts, true);
+  run = join_row<kWarps>(run, &space[0], 1 << lg_parts, true);
   float l;
   if (fabsf(run.m * c) < kFar) {
-    l = fmaf(fmaf(run.m, -c, run.K), kLn2, logf(run.s));
+    l = fmaf(fmaf(run.m, -c, float(run.K)), kLn2, logf(run.s));
   } else {
     // the whole row is far from zero (or infinite): once more, relative to the maximum
     Running far;
-    far.K = 0.f;
-    const int first = sp.head + sp.v0 * kN, last = sp.head + sp.v1 * kN;
-    const int edge = part == 0 ? sp.head : 0, tail = part == parts - 1 ? p.V - sp.tail0 : 0;
-    for (int i = tid; i < last - first + edge + tail; i += kThreads) {
-      const int e = i < edge ? i : i - edge < last - first ? first + i - edge : sp.tail0 + i - edge - (last - first);
+    far.K = 0;
+    const int first = sp.head + sp.v0 * kN, n = (sp.v1 - sp.v0) * kN;
+    for (int i = tid; i < n + sp.edge + sp.tail; i += kThreads) {
+      const int e = i < sp.edge ? i : i - sp.edge < n ? first + i - sp.edge : sp.tail0 + i - sp.edge - n;
       far.s += exp2f((Row<X>::one(row[e]) - run.m) * c);
     }
-    l = logf(join_row<kWarps>(far, part_of[1], warp_of[1], parts, false).s);
+    l = logf(join_row<kWarps>(far, &space[1], 1 << lg_parts, false).s);
   }
   if (l < 0.f) l = 0.f;   // (the maximum is one of the terms)
-  if (writes) {
-    if (tid == 0) stats[r] = make_float2(run.m / p.temperature, l);
+  if (part == 0) {
+    if (tid == 0) stats[u.r] = make_float2(run.m / p.temperature, l);
     for (int k = tid; k < u.n; k += kThreads) {
       const int t = token_of(p, u, k);
-      const long long y = id_of(p, t);
-      logp[t] = y < 0 ? 0.f : y >= p.V ? NAN : (Row<X>::one(row[y]) - run.m) / p.temperature - l;
+      const int y = u.n == 1 ? u.id : id_of(p, t);
+      logp[t] = y < 0 ? 0.f : y >= p.V ? NAN : ((k < kThreads ? own : Row<X>::one(row[y])) - run.m) / p.temperature - l;
     }
+  }
+}
+
+// `rows`: what a block of more than one warp looks over at once (with lg_parts == 0).
+template <typename X, int kWarps, int kUnroll>
+__global__ void __launch_bounds__(block_threads<kWarps>(), blocks_per_sm<kWarps, kUnroll>())
+token_logp_kernel(LogpArgs p, int lg_parts, int rows, float* logp, float2* stats) {
+  __shared__ JoinSpace space[2];
+  __shared__ Predicts found[kWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int part = kWarps == 1 ? 0 : blockIdx.x & ((1 << lg_parts) - 1), r = team_of<kWarps>(lg_parts);
+  if (kWarps == 1 && r >= p.T) return;
+  dependency_wait();
+  bool fine;
+  if (kWarps == 1 || rows == 1) {
+    const Predicts u = predicts_of(p, r, fine);
+    if (!fine || !row_used(p, u, part == 0 && (kWarps == 1 || warp == 0), logp, stats)) return;
+    if (kWarps > 1 && lg_parts) cooperative_groups::this_cluster().barrier_arrive();
+    token_logp_row<X, kWarps, kUnroll>(p, u, part, kWarps == 1 ? 0 : lg_parts, space, logp, stats);
+    return;
+  }
+  // a warp looks over a row, then the block takes those that predict something
+  const long long mine = r + (long long)warp * gridDim.x;   // (of neighbours mostly all predict something or none does)
+  if (warp < rows) {
+    Predicts u;
+    u.n = 0;
+    if (mine < p.T) {
+      u = predicts_of(p, int(mine), fine);
+      if (!fine || !row_used(p, u, true, logp, stats)) u.n = 0;
+    }
+    if (lane == 0) found[warp] = u;
+  }
+  __syncthreads();
+  for (int i = 0; i < rows; ++i) {
+    const Predicts u = found[i];
+    if (!u.n) continue;
+    token_logp_row<X, kWarps, kUnroll>(p, u, 0, 0, space, logp, stats);
+    __syncthreads();   // (the space of the sums is used again)
   }
 }
 
@@ -357,54 +417,63 @@ struct LogpBwdArgs {
 
 // kVec: rows of logits and of the gradient lie alike to 16 bytes.
 template <typename X, int kWarps, bool kVec>
-__global__ void __launch_bounds__(block_threads<kWarps>())
-token_logp_bwd_kernel(LogpArgs p, LogpBwdArgs b, int parts) {
-  constexpr int kN = Row<X>::kN, kThreads = kWarps * 32, kUnroll = 4;
-  dependency_wait();
-  if (p.header[0] != kStatusOk) return;
+__global__ void __launch_bounds__(block_threads<kWarps>(), blocks_per_sm<kWarps, 4>())
+token_logp_bwd_kernel(LogpArgs p, LogpBwdArgs b, int lg_parts) {
+  constexpr int kN = Row<X>::kN, kThreads = kWarps * 32, kUnroll = 4, kStep = kUnroll * kThreads;
+  if (kWarps == 1) lg_parts = 0;
   const int tid = kWarps == 1 ? threadIdx.x & 31 : threadIdx.x, lane = threadIdx.x & 31;
-  const int r = kWarps == 1 ? blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x / parts;
-  const int part = kWarps == 1 ? 0 : blockIdx.x % parts;
+  const int part = blockIdx.x & ((1 << lg_parts) - 1), r = team_of<kWarps>(lg_parts);
   if (r >= p.T) return;
-  const Predicts u = predicts_of(p, r);
+  dependency_wait();
+  const float next = b.grad[min(r + 1, p.T - 1)], next_logp = b.logp[min(r + 1, p.T - 1)];
+  const float2 st = b.stats[r];
+  bool fine;
+  const Predicts u = predicts_of(p, r, fine);
+  if (!fine) return;
   // the sum of the gradients of the tokens that the row predicts
   double total = 0;
   bool any = false;
-  for (int k = lane; k < u.n; k += 32) {
-    const int t = token_of(p, u, k);
-    if (id_of(p, t) >= 0) {
-      const float g = b.grad[t];
-      any |= g != 0.f;
-      total += g;
+  if (u.n == 1) {
+    if (u.id >= 0) {
+      total = next;
+      any = next != 0.f;
     }
-  }
-  any = __any_sync(0xffffffffu, any);
+  } else if (u.n > 1) {
+    for (int k = lane; k < u.n; k += 32) {
+      const int t = token_of(p, u, k);
+      if (id_of(p, t) >= 0) {
+        const float g = b.grad[t];
+        any |= g != 0.f;
+        total += g;
+      }
+    }
+    any = __any_sync(0xffffffffu, any);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+  }
 
   const X* row = static_cast<const X*>(p.logits) + (long long)r * p.row_stride;
   X* out = static_cast<X*>(b.d_logits) + (long long)r * b.d_stride;
-  const Span sp = span_of<X>(out, p.V, part, parts);
+  const Span sp = span_of<128>(out, p.V, part, lg_parts);
   uint4* dst = reinterpret_cast<uint4*>(out + sp.head);
-  const int edge = part == 0 ? sp.head : 0, tail = part == parts - 1 ? p.V - sp.tail0 : 0;
   if (!any) {
-    for (int i = tid; i < edge + tail; i += kThreads) Row<X>::store(out + (i < edge ? i : sp.tail0 + i - edge), 0.f);
+    for (int i = tid; i < sp.edge + sp.tail; i += kThreads)
+      Row<X>::store(out + (i < sp.edge ? i : sp.tail0 + i - sp.edge), 0.f);
     for (int at = sp.v0 + tid; at < sp.v1; at += kThreads) dst[at] = make_uint4(0, 0, 0, 0);
     return;
   }
   // p_v = 2^(c x_v - K) 2^-f with K + f = (m + l) log2(e), K whole: 2^-f goes into the row's factor
-  const float2 st = b.stats[r];
   const double lse2 = (double(st.x) + double(st.y)) * kLog2e;
   const double whole = rint(lse2);
   const bool far = !(fabs(lse2) < double(kFar));
-  const float scale = float(-total / double(p.temperature));
+  const float scale = -float(total) / p.temperature;
   const float coef = far ? scale : scale * exp2f(float(whole - lse2));
   const float K = float(whole), c = p.c;
   auto one = [&](float x) {
     return far ? scale * expf(x / p.temperature - st.x - st.y) : coef * ex2(fmaf(x, c, -K));
   };
-  for (int i = tid; i < edge + tail; i += kThreads) {
-    const int e = i < edge ? i : sp.tail0 + i - edge;
+  for (int i = tid; i < sp.edge + sp.tail; i += kThreads) {
+    const int e = i < sp.edge ? i : sp.tail0 + i - sp.edge;
     Row<X>::store(out + e, one(Row<X>::one(row[e])));
   }
   if (kVec && !far) {
@@ -425,15 +494,15 @@ token_logp_bwd_kernel(LogpArgs p, LogpBwdArgs b, int parts) {
       });
       return make_uint4(w[0], w[1], w[2], w[3]);
     };
-    int at = sp.v0 + tid;
-    uint4 v[kUnroll];
-    for (; at + (kUnroll - 1) * kThreads < sp.v1; at += kUnroll * kThreads) {
+    for (int at = sp.v0 + tid; at < sp.v1; at += kStep) {
+      uint4 v[kUnroll];
 #pragma unroll
-      for (int i = 0; i < kUnroll; ++i) v[i] = load_row(vec + at + i * kThreads);
+      for (int i = 0; i < kUnroll; ++i)
+        if (at + i * kThreads < sp.v1) v[i] = load_row(vec + at + i * kThreads);
 #pragma unroll
-      for (int i = 0; i < kUnroll; ++i) dst[at + i * kThreads] = take(v[i]);
+      for (int i = 0; i < kUnroll; ++i)
+        if (at + i * kThreads < sp.v1) dst[at + i * kThreads] = take(v[i]);
     }
-    for (; at < sp.v1; at += kThreads) dst[at] = take(load_row(vec + at));
   } else {
     for (int e = sp.head + sp.v0 * kN + tid; e < sp.head + sp.v1 * kN; e += kThreads)
       Row<X>::store(out + e, one(Row<X>::one(row[e])));
@@ -442,22 +511,23 @@ token_logp_bwd_kernel(LogpArgs p, LogpBwdArgs b, int parts) {
   // that of several responses: each writes the sum over all of them.
   row_sync<kWarps>();
   const int first = part == 0 ? 0 : sp.head + sp.v0 * kN;
-  const int last = part == parts - 1 ? p.V : sp.head + sp.v1 * kN;
+  const int last = part + 1 == 1 << lg_parts ? p.V : sp.head + sp.v1 * kN;
   for (int k = tid; k < u.n; k += kThreads) {
     const int t = token_of(p, u, k);
-    const long long y = id_of(p, t);
+    const int y = u.n == 1 ? u.id : id_of(p, t);
     if (y < first || y >= last) continue;
-    double same = 0;
-    if (u.n == 1) {
-      same = total;
-    } else {
+    float same = float(total), rest = 0.f, lp = next_logp;
+    if (u.n > 1) {
+      double sum = 0;
       for (int j = 0; j < u.n; ++j) {
         const int tj = token_of(p, u, j);
-        if (id_of(p, tj) == y) same += b.grad[tj];
+        if (id_of(p, tj) == y) sum += b.grad[tj];
       }
+      same = float(sum);
+      rest = float(total - sum);
+      lp = b.logp[t];
     }
-    const float lp = b.logp[t];
-    Row<X>::store(out + y, float((-same * double(expm1f(lp)) - (total - same) * double(expf(lp))) / double(p.temperature)));
+    Row<X>::store(out + y, (-same * expm1f(lp) - rest * expf(lp)) / p.temperature);
   }
 }
 
@@ -479,37 +549,66 @@ LogpArgs logp_args(const pp_plan* plan, const void* logits, long long row_stride
   return a;
 }
 
-// Warps per row and blocks per row.
+// How the rows are dealt out: warps of a row's team, blocks that share a row, rows that a block looks over,
+// vectors of a thread that are on their way at a time.  us on one B200, by bytes of a row and T rows:
+//  - a warp for a short row, where there are enough of them: 2.5 KB, T 37872 17 (4 warps 57); 16 KB, T 7867 18 (4 warps 22);
+//    but 7 KB, T 450 6.4 (4 warps 4.2).  It has two vectors of a row up to 4 KB on their way and 12 blocks on
+//    an SM, else four and 8: 2.5 KB 17.2 and 20.5, 16 KB 22.4 and 17.9.
+//  - 4 warps up to 32 KB, 8 beyond: 16 KB 22 and 33; 100 KB, T 990 backward 44 and 37.
+//  - forward, blocks that share a long row, where rows are few: 247 KB, T 242 17 (one), 12 (two), 9 (four); T 1020
+//    16 and 19, since the clusters of the rows that predict nothing have to be started too.
+//  - backward, parts of 64 to 112 KB: 257 KB, T 9241 573 (one), 567 (two), 555 (four); smaller parts where
+//    rows are few: 557 KB, T 165 47 (one), 36 (two), 29 (four).
+//  - forward, rows that a block looks over: about one of them predicts something, and there are at most sixteen waves of blocks:
+//    257 KB, T 65536 of which one in nine 384 (one), 317 (eight), one in three 351 and 264; T 20000, one in
+//    nine 119 and 100; but T 9241, every other one 194 and 217 (four).
 struct RowShape {
-  int warps, parts;
+  int warps, lg_parts, rows, unroll;
 };
-RowShape row_shape(int T, size_t row_bytes, int num_sms) {
-  RowShape s{16, 1};
-  if (row_bytes <= 8192) s.warps = 1;
-  else if (row_bytes <= 65536 && T >= 4 * num_sms) s.warps = 4;
-  if (s.warps == 16)
-    while (s.parts < kMaxParts && (long long)T * s.parts < 4ll * num_sms && row_bytes / (2 * s.parts) >= 8192) s.parts *= 2;
+RowShape row_shape(const pp_plan* plan, size_t row_bytes, int num_sms, bool fwd) {
+  const long long T = plan->prob.total_tokens;
+  RowShape s{8, 0, 1, 4};
+  if (row_bytes <= (T > 32ll * num_sms ? 16384 : T > 8ll * num_sms ? 4096 : 0)) {
+    s.warps = 1;
+    if (row_bytes <= 4096 && fwd) s.unroll = 2;
+    return s;
+  }
+  if (row_bytes <= 32768) s.warps = 4;
+  if (fwd) {
+    if (s.warps == 8)
+      while (s.lg_parts < kMaxLgParts && (T << (s.lg_parts + 1)) <= 7ll * num_sms && row_bytes >> (s.lg_parts + 1) >= 49152)
+        ++s.lg_parts;
+    // rows that predict something: all but the last of a response, and one of a prompt
+    const long long used = plan->resp_tokens - plan->prob.num_responses + plan->prob.num_groups;
+    const long long rows = std::max(plan->resp_tokens ? T / std::max(used, 1ll) : 0, T / (16ll * (32 / s.warps) * num_sms));
+    if (T > 7ll * num_sms) s.rows = int(std::max(1ll, std::min(rows, (long long)s.warps)));
+  } else if (s.warps == 8) {
+    auto few = [&](int lg) { return (T << (lg + 1)) <= 4ll * num_sms && row_bytes >> (lg + 1) >= 16384; };
+    while (s.lg_parts < kMaxLgParts && (row_bytes >> s.lg_parts > 114688 || few(s.lg_parts))) ++s.lg_parts;
+  }
   return s;
 }
+dim3 blocks_of(int T, RowShape s) {
+  return dim3(s.warps == 1 ? unsigned((T + 3ll) / 4) : s.rows > 1 ? unsigned((T + s.rows - 1ll) / s.rows) : unsigned(T) << s.lg_parts);
+}
+dim3 threads_of(RowShape s) { return dim3(s.warps == 1 ? 128 : s.warps * 32); }
 
 template <typename X>
 cudaError_t launch_fwd_of(const LogpArgs& a, RowShape s, float* logp, float2* stats, cudaStream_t stream) {
-  if (s.warps == 1)
-    return launch_kernel(true, token_logp_kernel<X, 1>, dim3((a.T + 7) / 8), dim3(256), 0, stream, a, 1, logp, stats);
-  if (s.warps == 4)
-    return launch_kernel(true, token_logp_kernel<X, 4>, dim3(a.T), dim3(128), 0, stream, a, 1, logp, stats);
-  return launch_clusters(s.parts, token_logp_kernel<X, 16>, dim3(unsigned(a.T) * s.parts), dim3(512), 0, stream, a,
-                         s.parts, logp, stats);
+  auto kernel = s.warps == 8    ? token_logp_kernel<X, 8, 4>
+                : s.warps == 4  ? token_logp_kernel<X, 4, 4>
+                : s.unroll == 4 ? token_logp_kernel<X, 1, 4>
+                                : token_logp_kernel<X, 1, 2>;
+  return launch_clusters(1 << s.lg_parts, kernel, blocks_of(a.T, s), threads_of(s), 0, stream, a, s.lg_parts, s.rows,
+                         logp, stats);
 }
 
 template <typename X, bool kVec>
 cudaError_t launch_bwd_of(const LogpArgs& a, RowShape s, const LogpBwdArgs& b, cudaStream_t stream) {
-  if (s.warps == 1)
-    return launch_kernel(true, token_logp_bwd_kernel<X, 1, kVec>, dim3((a.T + 7) / 8), dim3(256), 0, stream, a, b, 1);
-  if (s.warps == 4)
-    return launch_kernel(true, token_logp_bwd_kernel<X, 4, kVec>, dim3(a.T), dim3(128), 0, stream, a, b, 1);
-  return launch_kernel(true, token_logp_bwd_kernel<X, 16, kVec>, dim3(unsigned(a.T) * s.parts), dim3(512), 0, stream, a,
-                       b, s.parts);
+  auto kernel = s.warps == 8   ? token_logp_bwd_kernel<X, 8, kVec>
+                : s.warps == 4 ? token_logp_bwd_kernel<X, 4, kVec>
+                               : token_logp_bwd_kernel<X, 1, kVec>;
+  return launch_kernel(true, kernel, blocks_of(a.T, s), threads_of(s), 0, stream, a, b, s.lg_parts);
 }
 
 size_t size_of(int type) { return type == PP_FP32 ? 4 : 2; }
@@ -523,7 +622,7 @@ cudaError_t launch_token_logp(const pp_plan* plan, const void* logits, int type,
   const DeviceSetup* dev = device_setup(setup);
   if (!dev) return cudaErrorInvalidDevice;
   const LogpArgs a = logp_args(plan, logits, row_stride, V, ids, ids_64, temperature);
-  const RowShape s = row_shape(a.T, size_t(V) * size_of(type), dev->num_sms);
+  const RowShape s = row_shape(plan, size_t(V) * size_of(type), dev->num_sms, true);
   float2* st = reinterpret_cast<float2*>(stats);
   return type == PP_BF16   ? launch_fwd_of<__nv_bfloat16>(a, s, logp, st, stream)
          : type == PP_FP16 ? launch_fwd_of<__half>(a, s, logp, st, stream)
@@ -539,7 +638,7 @@ cudaError_t launch_token_logp_bwd(const pp_plan* plan, const void* logits, int t
   if (!dev) return cudaErrorInvalidDevice;
   const LogpArgs a = logp_args(plan, logits, row_stride, V, ids, ids_64, temperature);
   const LogpBwdArgs b{logp, reinterpret_cast<const float2*>(stats), grad, d_logits, d_stride};
-  const RowShape s = row_shape(a.T, size_t(V) * size_of(type), dev->num_sms);
+  const RowShape s = row_shape(plan, size_t(V) * size_of(type), dev->num_sms, false);
   const long long apart = reinterpret_cast<const char*>(logits) - static_cast<char*>(d_logits);
   const bool vec = apart % 16 == 0 && (row_stride - d_stride) * (long long)size_of(type) % 16 == 0;
   auto go = [&](auto x) {

@@ -138,6 +138,57 @@ def test_parity_of_large_vocabularies(tokens, V, kind):
     _check_bwd(rows, logits, ids, g, 1.0, d, kind)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("V", [600, 9001, 20000])
+def test_parity_of_mostly_prompts(V, kind):
+    """Blocks that look over several rows at once, of which few predict something."""
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(1200, (40, 30, 9))], [(90, (3,)), (1, (1, 2))]]
+    logits, ids, _ = _inputs(rows, V, TYPES[kind][0], 7)
+    ids[[1200, 1370]] = -1
+    used = sorted({r for r, t in P.predictions(rows) if ids[t] >= 0})
+    logits[[i for i in range(len(ids)) if i not in set(used)]] = float("nan")      # not read
+    g = torch.randn(len(ids), generator=torch.Generator().manual_seed(5)).cuda()
+    for on_device in (False, True):
+        plan = _plan(rows, desc_on_device=on_device)
+        logp, stats = B.pp_token_logp(plan, logits, ids)
+        d = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g)
+        assert plan.status() == (0, 0)
+        safe = torch.nan_to_num(logits)
+        _check_fwd(rows, safe, ids, 1.0, logp, stats)
+        _check_bwd(rows, safe, ids, g, 1.0, d, kind)
+
+
+@pytest.mark.parametrize("V", [257, 3000])
+def test_parity_of_many_short_rows(V):
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(2, (30, 31)), (40, (1, 2, 3))]] * 48
+    logits, ids, _ = _inputs(rows, V, torch.bfloat16, 9)
+    assert len(ids) > 32 * 148
+    plan = _plan(rows)
+    g = torch.randn(len(ids), generator=torch.Generator().manual_seed(5)).cuda()
+    logp, stats = B.pp_token_logp(plan, logits, ids)
+    d = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g)
+    _check_fwd(rows, logits, ids, 1.0, logp, stats)
+    _check_bwd(rows, logits, ids, g, 1.0, d, "bf16")
+
+
+@pytest.mark.parametrize("T,V", [(20000, 17000), (40000, 5001)])
+def test_the_way_rows_are_dealt_out_does_not_change_them(T, V):
+    """A plan from host arrays knows how many tokens the responses hold, one from device arrays does not: their
+    blocks look over other numbers of rows."""
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(T - 310, (200, 7))], [(2, (1, 100))]]
+    g = torch.Generator(device="cuda").manual_seed(0)
+    logits = torch.randn(T, V, generator=g, device="cuda", dtype=torch.bfloat16)
+    ids = torch.randint(0, V, (T,), generator=g, device="cuda")
+    a, b = (B.pp_token_logp(_plan(rows, desc_on_device=d), logits, ids) for d in (False, True))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and a[0].count_nonzero() > 300
+    r, t = (torch.tensor(x, device="cuda") for x in zip(*P.predictions(rows)))
+    want = torch.log_softmax(logits[r].double(), -1)[torch.arange(len(t), device="cuda"), ids[t]]
+    assert float((a[0][t].double() - want).abs().max()) < U * (600 + 8 * 12 + 8 * 30)
+
+
 @pytest.mark.parametrize("V,kind", [(100, "fp32"), (4099, "bf16"), (20000, "fp16"), (60000, "fp32"), (140000, "bf16")])
 def test_masked_and_extreme_logits(V, kind):
     from paper_2602_24082_b200 import binding as B
@@ -174,7 +225,7 @@ def test_masked_and_extreme_logits(V, kind):
     nan = np.isnan(want)
     assert np.array_equal(np.isnan(got), nan)
     fine = np.isfinite(want)
-    assert (np.abs(got - want)[fine] <= U * (600 + 8 * np.log(V) + 8 * np.abs(want[fine]))).all()
+    assert (np.abs(got[fine] - want[fine]) <= U * (600 + 8 * np.log(V) + 8 * np.abs(want[fine]))).all()
     # gradients of the rows that are numbers
     g = torch.randn(len(ids), generator=torch.Generator().manual_seed(5)).cuda()
     g[torch.from_numpy(nan).cuda()] = 0
