@@ -157,6 +157,7 @@ class Plan:
         self._problem: Optional[_Problem] = None
         self._sizes: Optional[Tuple[int, int, int]] = None
         self._bwd_scratch: Optional[torch.Tensor] = None
+        self._num_responses: Optional[int] = None
         self.total_tokens = total_tokens
         # the arguments every call of a step starts with
         self._head = (handle, total_tokens, num_q_heads, num_kv_heads, head_dim)
@@ -167,6 +168,12 @@ class Plan:
             _, T, Hq, Hkv, D = self._head
             self._problem, self._keep = make_problem(self._keep[0], Hq, Hkv, D, T, self._keep[1])
         return self._problem
+
+    @property
+    def num_responses(self) -> int:
+        if self._num_responses is None:
+            self._num_responses = self.problem.num_responses
+        return self._num_responses
 
     q_shape = property(lambda self: (self._head[1], self._head[2], self._head[4]))
     kv_shape = property(lambda self: (self._head[1], self._head[3], self._head[4]))
@@ -438,7 +445,7 @@ def pp_policy_loss(plan: Plan, token_logp: torch.Tensor, old_token_logp: Optiona
         raise ValueError(f"advantage: expected one of {', '.join(_ADVANTAGES)}, got {advantage!r}")
     if reduction not in _REDUCTIONS:
         raise ValueError(f"reduction: expected one of {', '.join(_REDUCTIONS)}, got {reduction!r}")
-    return _step_calls().policy_loss(plan.handle, plan.workspace, plan.total_tokens, plan.problem.num_responses,
+    return _step_calls().policy_loss(plan.handle, plan.workspace, plan.total_tokens, plan.num_responses,
                                      token_logp, old_token_logp, ref_token_logp, reward, token_mask,
                                      _ADVANTAGES[advantage], _REDUCTIONS[reduction], clip_low, clip_high, kl_coef,
                                      scale, eps, want_grad)

@@ -396,6 +396,14 @@ struct Around {
                          const char* name) const {
     return ::take(o, type, type_name, shape, name, ws, "the plan");
   }
+  // a new tensor [sizes] of 4-byte elements at element `at` of a buffer that several outputs share (an allocation, and each
+  // view of it made through the dispatcher, takes as long as all the rest of a call)
+  static at::Tensor piece(const at::Tensor& buffer, int64_t at, at::IntArrayRef sizes) {
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(buffer.storage()), buffer.key_set(), buffer.dtype());
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+    t.unsafeGetTensorImpl()->set_storage_offset(at);
+    return t;
+  }
   // a given output, or a new one
   bool out(at::Tensor& to, PyObject* o, at::ScalarType type, const char* type_name, at::IntArrayRef shape,
            const char* name) const {
@@ -423,9 +431,15 @@ PyObject* position_ids_axes(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !(grid = c.take(a[5], at::kInt, "int32", {I, 3}, "span_grid")))
     return nullptr;
   const c10::cuda::CUDAGuard guard(c.ws->device());
-  at::Tensor out;
-  if (!c.out(out, a[6], at::kInt, "int32", {3, T}, "position_ids")) return nullptr;
-  const at::Tensor status = at::empty({2}, start->options());
+  at::Tensor out, status;
+  if (a[6] == Py_None) {
+    const at::Tensor both = at::empty({3 * T + 2}, start->options());
+    out = Around::piece(both, 0, {3, T});
+    status = Around::piece(both, 3 * T, {2});
+  } else {
+    if (!c.out(out, a[6], at::kInt, "int32", {3, T}, "position_ids")) return nullptr;
+    status = at::empty({2}, start->options());
+  }
   const int rc = api.position_ids_axes(c.plan, int32_t(I), start->data_ptr<int32_t>(), grid->data_ptr<int32_t>(),
                                        out.data_ptr<int32_t>(), status.data_ptr<int32_t>(), c.stream());
   if (rc) return raise_code(rc, "pp_position_ids_axes");
@@ -519,8 +533,14 @@ PyObject* token_logp(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!(x = take_logits(a[3], c, T, nullptr, "logits")) || !(ids = take_ids(a[4], c, T))) return nullptr;
   const c10::cuda::CUDAGuard guard(c.ws->device());
   at::Tensor logp, stats;
-  if (!c.out(logp, a[6], kF32, "float32", {T}, "token_logp") || !c.out(stats, a[7], kF32, "float32", {T, 2}, "row_stats"))
+  if (a[6] == Py_None && a[7] == Py_None) {
+    const at::Tensor both = at::empty({3 * T}, c.ws->options().dtype(kF32));
+    stats = Around::piece(both, 0, {T, 2});
+    logp = Around::piece(both, 2 * T, {T});
+  } else if (!c.out(logp, a[6], kF32, "float32", {T}, "token_logp") ||
+             !c.out(stats, a[7], kF32, "float32", {T, 2}, "row_stats")) {
     return nullptr;
+  }
   const int rc = api.token_logp(c.plan, x->data_ptr(), dtype_of(*x), row_stride(*x), int32_t(x->size(1)),
                                 ids->data_ptr(), ids->scalar_type() == at::kLong, float(temperature),
                                 logp.data_ptr<float>(), stats.data_ptr<float>(), c.stream());
@@ -592,21 +612,19 @@ PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
       (a[8] != Py_None && !(mask = c.take(a[8], at::kBool, "bool", {T}, "token_mask"))))
     return nullptr;
   const c10::cuda::CUDAGuard guard(c.ws->device());
-  // (one allocation for the numbers per response)
-  const int64_t row = (N + 3) / 4 * 4;
-  const at::Tensor per_resp = at::empty({per_token ? 3 : 4, row}, logp->options());
-  const at::Tensor grad = want ? at::empty({T}, logp->options()) : at::Tensor();
-  float* r = per_resp.data_ptr<float>();
+  const int64_t row = (N + 3) / 4 * 4, rows = per_token ? 3 : 4;
+  const at::Tensor all = at::empty({rows * row + (want ? T : 0)}, logp->options());
+  float* r = all.data_ptr<float>();
   auto f = [](const at::Tensor* t) { return t ? t->data_ptr<float>() : nullptr; };
   const int rc = api.policy_loss(c.plan, &o, f(logp), f(old), f(ref), f(reward),
                                  mask ? static_cast<const uint8_t*>(mask->data_ptr()) : nullptr,
                                  per_token ? nullptr : r + 3 * row, r, r + row, r + 2 * row,
-                                 want ? grad.data_ptr<float>() : nullptr, c.stream());
+                                 want ? r + rows * row : nullptr, c.stream());
   if (rc) return raise_code(rc, "pp_policy_loss");
-  auto part = [&](int64_t i) { return THPVariable_Wrap(per_resp.select(0, i).narrow(0, 0, N)); };
+  auto part = [&](int64_t i, int64_t n) { return THPVariable_Wrap(Around::piece(all, i * row, {n})); };
   auto none = [] { Py_INCREF(Py_None); return Py_None; };
-  return Py_BuildValue("(NNNNN)", part(0), part(1), part(2), per_token ? none() : part(3),
-                       want ? THPVariable_Wrap(grad) : none());
+  return Py_BuildValue("(NNNNN)", part(0, N), part(1, N), part(2, N), per_token ? none() : part(3, N),
+                       want ? part(rows, T) : none());
   PP_GUARD_END
 }
 
