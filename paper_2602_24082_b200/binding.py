@@ -402,7 +402,8 @@ def pp_rope_qk_axes(plan: Plan, q: torch.Tensor, k: torch.Tensor, position_ids: 
     ``q_out`` / ``k_out``; q, k and the outputs may be views of a fused projection's buffer.
     ``sections``: how many of the D / 2 frequencies each axis has (see ``axis_of_frequency``).
     ``inverse``: the backward pass, on dQ and dK.  Returns (q_out, k_out)."""
-    axis = axis_of_frequency(tuple(sections), bool(interleaved))
+    sections = tuple(sections)
+    axis = axis_of_frequency(sections, bool(interleaved))
     handle, T, Hq, Hkv, D = plan._head
     return _step_calls().rope_qk_axes(handle, plan.workspace, T, Hq, Hkv, D, q, k, position_ids, len(sections), axis,
                                       rope_base, inverse, q_out, k_out)

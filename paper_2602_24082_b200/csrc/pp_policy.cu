@@ -89,11 +89,11 @@ __global__ void __launch_bounds__(kThreads) policy_loss_kernel(PolicyArgs p, int
   if (kTeam == kThreads && parts > 1) cooperative_groups::this_cluster().barrier_arrive();
   const int status = p.header[0];
   const int g = warp_upper(p.grp_resp_off, p.G, x);
+  if (status != kStatusOk) return;   // (a refused plan's offsets may point anywhere)
   const int seg = g + 1 + x;
   const int a = p.seg_start[seg], b = p.seg_start[seg + 1];
   const int x0 = p.grp_resp_off[g], n = p.grp_resp_off[g + 1] - x0, sp = g + x0;
   const int p0 = p.seg_start[sp], p1 = p.seg_start[sp + 1];
-  if (status != kStatusOk) return;
   const int stride = kTeam * parts, first = a + part * kTeam + in_team;
   const bool per_token = p.o.advantage_mode == PP_ADVANTAGE_TOKEN;
   // what a token needs; that of a thread's first is on its way while the advantage and the count are found

@@ -147,3 +147,60 @@ def test_the_preference_loss_takes_the_same_log_probabilities():
     # the loss is within 1e-4 (its own test), its gradient too; the logits' is a sum of products with it
     assert abs(float(loss.double().sum() - total.detach())) < 1e-4 * float(total.detach())
     assert float((d.double() - leaf.grad).norm() / leaf.grad.norm()) < 2e-4
+
+
+@pytest.mark.parametrize("broken", ["offset", "length", "tokens"])
+def test_a_refused_plan_leaves_the_outputs_as_they_were(broken):
+    """Descriptors that only the device sees: the plan's status says so, and the calls around it read and write nothing by
+    them.  (Offsets that point far outside among them.)"""
+    from paper_2602_24082_b200 import binding as B
+    rgo, gpl, gro, rl = [np.asarray(a, np.int32) for a in ([0, 1, 2], [5, 7], [0, 2, 3], [4, 3, 6])]
+    if broken == "offset":
+        gro[1] = 2000000000
+    elif broken == "length":
+        rl[1] = -2000000000
+    else:
+        gpl[0] = 6
+    plan = B.pp_build_plan((rgo, gpl, gro, rl), 2, 1, 64, 25, desc_on_device=True)
+    f = lambda *shape: torch.full(shape, 7.0, device="cuda")
+    ids = torch.zeros(25, dtype=torch.int64, device="cuda")
+    logp, stats, d = f(25), f(25, 2), f(25, 99)
+    B.pp_token_logp(plan, f(25, 99), ids, token_logp=logp, row_stats=stats)
+    B.pp_token_logp_bwd(plan, f(25, 99), ids, f(25), f(25, 2), f(25), d_logits=d)
+    q, k = f(25, 2, 64).bfloat16(), f(25, 1, 64).bfloat16()
+    pos = torch.full((3, 25), 7, dtype=torch.int32, device="cuda")
+    B.pp_position_ids_axes(plan, pos[0, :1].contiguous(), pos[:1, :3].contiguous(), out=pos)
+    B.pp_rope_qk_axes(plan, q, k, pos, (8, 12, 12))
+    B.pp_policy_loss(plan, f(25), f(25), f(25), f(3))
+    torch.cuda.synchronize()
+    assert plan.status()[0] in (1, 2)
+    assert all((x == 7).all() for x in (logp, stats, d, q, k, pos))
+
+
+def test_calls_of_two_streams_on_one_plan():
+    """None of the calls around the attention changes the plan: they may run at the same time."""
+    from paper_2602_24082_b200 import binding as B
+    w = W.Workload("two", [[(300, (200, 100))], [(500, (40, 300, 77))]] * 4, 8, 2, 64, seed=0)
+    T = w.total_tokens
+    plan = B.plan_for(w)
+    g = torch.Generator(device="cuda").manual_seed(0)
+    data = []
+    for _ in range(2):
+        logits = torch.randn(T, 5000, generator=g, device="cuda")
+        data.append((logits, torch.randint(0, 5000, (T,), generator=g, device="cuda"), torch.randn(20, generator=g, device="cuda")))
+
+    def work(logits, ids, reward):
+        logp, stats = B.pp_token_logp(plan, logits, ids)
+        loss, _, _, _, d_logp = B.pp_policy_loss(plan, logp, None, None, reward, kl_coef=0.1)
+        return loss, B.pp_token_logp_bwd(plan, logits, ids, logp, stats, d_logp)
+
+    want = [work(*x) for x in data]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in data]
+    got = [None, None]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = work(*data[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
