@@ -12,13 +12,17 @@
 // Rows that predict nothing are not read; their gradient is zero.
 //
 // Both passes are bound by HBM: the forward reads a predicting row once, with the running maximum and sum of a
-// softmax, the backward reads and writes it once.  What keeps the forward at the memory's rate
-// is one exponential per element and little else: 128 K columns of bf16 at 6.5 TB/s are 11.7 elements per clock
-// and SM, of 16 that the special function unit makes.  The exponential is 2^(c x - K), c = log2(e) /
-// temperature, with a whole number K >= c max(x) for reference: K is exact in fp32, so nothing of c x is
+// softmax, the backward reads and writes it once.  9241 rows of 128256 bf16 columns, 4935 of which predict something: 1.27 GB
+// in 194 us (6.5 TB/s, as a copy), the gradient 3.64 GB in 554 (6.6).  What keeps the forward at the memory's rate
+// is one exponential per element and little else: bf16 at 6.5 TB/s are 11.7 elements per clock
+// and SM, of 16 that the special function unit makes (measured busy for 77 %).  The exponential is 2^(c x - K), c = log2(e) /
+// temperature, with a whole number K for reference: K is exact in fp32, so nothing of c x is
 // lost to the rounding of a reference (c m rounded would be off by 2^-24 |c m|, the same for the whole
-// row), sums of different references are joined by exact powers of two, and a larger element than those
-// seen so far costs one multiplication, rarely.  A thread takes four 16-byte vectors at a time.
+// row), and sums of different references are joined by exact powers of two.  K comes from a thread's first elements and
+// stays unless one is 2^64 times as large: a new reference with every new maximum was a branch that some lane of
+// a warp took in nearly every step (128 instead of 99 million instructions; under the power limit of a long run, at
+// 1.7 GHz, 219 us instead of 201 - 210).  A thread has four 16-byte vectors on their way while it sums up four
+// (without that 252 us).
 // Rows whose values are beyond +-2^19 (a mask of the type's lowest value over everything, say)
 // go through a second pass over exp(x - m).
 #include <cooperative_groups.h>
@@ -33,6 +37,7 @@ namespace {
 
 constexpr float kFar = 524288.f;   // |c m| up to which ceil(c m) is at most 1 above c m
 constexpr int kMostK = 1 << 20;
+constexpr float kSlack = 64.f;     // powers up to 2^64 are summed up: 2^95 with the longest row
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr double kLog2e = 1.4426950408889634074;
 
@@ -201,6 +206,9 @@ __device__ __forceinline__ int whole(float cm) { return int(fminf(fmaxf(ceilf(cm
 __device__ __forceinline__ float power(int from, int to) {   // 2^(from - to), from <= to: exact, and 0 far below
   return __int_as_float(max(127 + from - to, 0) << 23);
 }
+__device__ __forceinline__ float power2(int n) {   // 2^n, |n| < 127
+  return __int_as_float((127 + n) << 23);
+}
 // floats in the order of signed whole numbers, and back
 __device__ __forceinline__ int ordered(float x) {
   const int i = __float_as_int(x);
@@ -299,15 +307,16 @@ __device__ __forceinline__ void token_logp_row(const LogpArgs& p, const Predicts
   }
   Running run;
   uint64_t sum = pack2(0.f, 0.f);
+  float k = float(kMostK);   // -K
   auto raise = [&](float bm) {
-    const int K = whole(bm * c);
     run.m = fmaxf(run.m, bm);
-    if (K > run.K) {
+    if (fmaf(bm, c, k) > kSlack) {
+      const int K = whole(bm * c);
       const float f = power(run.K, K);
       sum = mul2(sum, pack2(f, f));
       run.K = K;
+      k = -float(K);
     }
-    return -float(run.K);
   };
   auto take = [&](const uint4 (&v)[kUnroll], int n) {   // (n: vectors that some thread has)
     uint32_t w = Row<X>::max_word(Row<X>::max_word(v[0].x, v[0].y), Row<X>::max_word(v[0].z, v[0].w));
@@ -315,7 +324,7 @@ __device__ __forceinline__ void token_logp_row(const LogpArgs& p, const Predicts
     for (int i = 1; i < kUnroll; ++i)
       if (kWarps > 1 || i < n)
         w = Row<X>::max_word(w, Row<X>::max_word(Row<X>::max_word(v[i].x, v[i].y), Row<X>::max_word(v[i].z, v[i].w)));
-    const float k = raise(Row<X>::max_of(w));
+    raise(Row<X>::max_of(w));
     const uint64_t k2 = pack2(k, k);
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i)
@@ -329,11 +338,25 @@ __device__ __forceinline__ void token_logp_row(const LogpArgs& p, const Predicts
   // elements in front of the first boundary and behind the last, one per thread
   for (int i = tid; i < sp.edge + sp.tail; i += kThreads) {
     const float x = Row<X>::one(row[i < sp.edge ? i : sp.tail0 + i - sp.edge]);
-    const float k = raise(x);
+    raise(x);
     sum = add2(sum, pack2(ex2(fmaf(x, c, k)), 0.f));
   }
-  // one batch of vectors is on its way while the one before it is summed up
-  for (int at = sp.v0; at < sp.v1; at += 2 * kStep) {
+  // one batch of vectors is on its way while the one before it is summed up; of a long row, while there are whole
+  // ones, without a look at where it ends
+  int at = sp.v0;
+  if constexpr (kWarps > 1) {
+    auto load_whole = [&](uint4 (&v)[kUnroll], int at) {
+#pragma unroll
+      for (int i = 0; i < kUnroll; ++i) v[i] = load_row(vec + at + i * kThreads);
+    };
+    for (; at + 3 * kStep <= sp.v1; at += 2 * kStep) {
+      load_whole(vb, at + tid + kStep);
+      take(va, kUnroll);
+      load_whole(va, at + tid + 2 * kStep);
+      take(vb, kUnroll);
+    }
+  }
+  for (; at < sp.v1; at += 2 * kStep) {
     load(vb, at + tid + kStep);
     take(va, (sp.v1 - at + kThreads - 1) / kThreads);
     load(va, at + tid + 2 * kStep);
@@ -345,7 +368,8 @@ __device__ __forceinline__ void token_logp_row(const LogpArgs& p, const Predicts
   run = join_row<kWarps>(run, &space[0], 1 << lg_parts, true);
   float l;
   if (fabsf(run.m * c) < kFar) {
-    l = fmaf(fmaf(run.m, -c, float(run.K)), kLn2, logf(run.s));
+    const int K = whole(run.m * c);
+    l = fmaf(fmaf(run.m, -c, float(K)), kLn2, logf(run.s * power2(run.K - K)));
   } else {
     // the whole row is far from zero (or infinite): once more, relative to the maximum
     Running far;
@@ -417,7 +441,7 @@ struct LogpBwdArgs {
 
 // kVec: rows of logits and of the gradient lie alike to 16 bytes.
 template <typename X, int kWarps, bool kVec>
-__global__ void __launch_bounds__(block_threads<kWarps>(), blocks_per_sm<kWarps, 4>())
+__global__ void __launch_bounds__(block_threads<kWarps>(), kWarps == 1 ? 10 : blocks_per_sm<kWarps, 4>())
 token_logp_bwd_kernel(LogpArgs p, LogpBwdArgs b, int lg_parts) {
   constexpr int kN = Row<X>::kN, kThreads = kWarps * 32, kUnroll = 4, kStep = kUnroll * kThreads;
   if (kWarps == 1) lg_parts = 0;
@@ -478,13 +502,12 @@ token_logp_bwd_kernel(LogpArgs p, LogpBwdArgs b, int lg_parts) {
   }
   if (kVec && !far) {
     const uint4* vec = reinterpret_cast<const uint4*>(row + sp.head);
-    const uint64_t c2 = pack2(c, c), k2 = pack2(-K, -K), f2 = pack2(coef, coef);
     auto take = [&](uint4 v) {
       uint32_t w[4];
       int i = 0;
       for_pairs<X>(v, [&](float x, float y) {
-        unpack2(fma2(pack2(x, y), c2, k2), x, y);
-        unpack2(mul2(pack2(ex2(x), ex2(y)), f2), x, y);
+        x = ex2(fmaf(x, c, -K)) * coef;
+        y = ex2(fmaf(y, c, -K)) * coef;
         if constexpr (kN == 8) {
           w[i++] = Row<X>::word(x, y);
         } else {
@@ -553,7 +576,7 @@ LogpArgs logp_args(const pp_plan* plan, const void* logits, long long row_stride
 // vectors of a thread that are on their way at a time.  us on one B200, by bytes of a row and T rows:
 //  - a warp for a short row, where there are enough of them: 2.5 KB, T 37872 17 (4 warps 57); 16 KB, T 7867 18 (4 warps 22);
 //    but 7 KB, T 450 6.4 (4 warps 4.2).  It has two vectors of a row up to 4 KB on their way and 12 blocks on
-//    an SM, else four and 8: 2.5 KB 17.2 and 20.5, 16 KB 22.4 and 17.9.
+//    an SM, else four and 8: 2.5 KB 17.2 and 20.5, 16 KB 22.4 and 17.9.  (Backward, 10 blocks: 3 KB, T 61100 74, with 8 78.)
 //  - 4 warps up to 32 KB, 8 beyond: 16 KB 22 and 33; 100 KB, T 990 backward 44 and 37.
 //  - forward, blocks that share a long row, where rows are few: 247 KB, T 242 17 (one), 12 (two), 9 (four); T 1020
 //    16 and 19, since the clusters of the rows that predict nothing have to be started too.

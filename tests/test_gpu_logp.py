@@ -80,7 +80,12 @@ def _check_bwd(rows, logits, ids, grad, temperature, d, kind):
     top = np.where(np.isfinite(x).any(1), np.where(np.isfinite(x), x, -np.inf).max(1), 0)
     E = np.abs(top / temp) * 1.4427
     E = np.where(E < 2.0 ** 19, E, 0) + np.log2(x.shape[1] + 1)      # (beyond, exp(x - m - l) itself is taken)
-    tol = half * np.abs(want) * (1 + 2 * half) + U * (700 + 8 * E)[:, None] * size + tiny
+    # the power 2^(c x - K) is 0 below 2^-126 (flushed); the row's factor, at most the sum of |g| / temperature times
+    # 2^(1/2) for the fraction taken off with K, multiplies it: that much is lost, whatever the type
+    weight = np.zeros(len(x))
+    np.add.at(weight, [r for r, _ in P.predictions(rows)], np.abs(_f64(grad))[[t for _, t in P.predictions(rows)]])
+    flushed = 2.0 ** -126 * 1.4143 * weight / temp
+    tol = half * np.abs(want) * (1 + 2 * half) + U * (700 + 8 * E)[:, None] * size + tiny + flushed[:, None]
     err = np.abs(_f64(d) - want)
     assert (err <= tol).all(), (err / tol).max()
 
@@ -234,6 +239,39 @@ def test_masked_and_extreme_logits(V, kind):
     safe = torch.where(torch.isnan(x) | (x == float("inf")), torch.zeros_like(x), x)
     safe[8] = 0
     _check_bwd(rows, safe, ids, g, 1.0, d, kind)
+
+
+@pytest.mark.parametrize("V", [300, 5000, 20000, 140000])
+def test_rows_that_rise_fall_and_jump(V):
+    """A thread's reference comes from its first elements: rows whose later ones are larger by less and by more than
+    the 2^64 that it may stay for, at the end, in the middle, everywhere."""
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(1, (12, 9))]]
+    logits, ids, _ = _inputs(rows, V, torch.float32, 3)
+    x, n = logits, torch.linspace(0, 1, V, device="cuda")
+    x[0] = 800 * n - 400
+    x[1] = 400 - 800 * n
+    x[2] = -30.0 + 1e-3 * x[2]
+    x[2, V - 1] = 12.0                  # 2^61 times as large
+    x[3] = -30.0 + 1e-3 * x[3]
+    x[3, V // 2] = 17.0                 # 2^68
+    x[4] = -3000.0 * (n < 0.5) + 0.01 * x[4]
+    x[5] = -60.0 * (1 - n)
+    x[6] = 1000 * torch.sin(40 * n)
+    x[7] = 0.0
+    x[8] = torch.where(torch.arange(V, device="cuda") % 2 == 0, 44.0, -44.0)
+    x[9, : V - 1] = -float("inf")
+    x[10] = -float("inf")
+    x[10, V // 3] = 300000.0
+    x[11, 0] = 3000.0
+    for t, y in ((2, V - 1), (3, V - 1), (4, V // 2), (5, V - 1), (10, V - 1), (11, V // 3), (14, 0)):
+        ids[t] = y
+    plan = _plan(rows)
+    logp, stats = B.pp_token_logp(plan, logits, ids)
+    g = torch.randn(len(ids), generator=torch.Generator().manual_seed(5)).cuda()
+    d = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g)
+    _check_fwd(rows, logits, ids, 1.0, logp, stats)
+    _check_bwd(rows, logits, ids, g, 1.0, d, "fp32")
 
 
 @pytest.mark.parametrize("V", [50, 5000, 70000])
