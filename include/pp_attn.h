@@ -229,7 +229,9 @@ int pp_preference_loss(const pp_plan* plan, const float* token_logp, const float
 /*
  * The steps of a training step on image prompts and on rewards, around the same packed layout.  All of them
  * need only a plan for the same descriptors, are one kernel on `stream`, and take DEVICE
- * pointers; results do not depend on the order in which blocks run.
+ * pointers; results do not depend on the order in which blocks run.  They leave the plan as it is: calls on one
+ * plan may overlap with each other and with the attention.  With a plan that the device has refused
+ * (pp_plan_status) they write nothing.
  *
  * Position ids with a time, a height and a width axis (the paper trains on image prompts, Sec. 4).  A
  * token of text has the running number n of its unpacked sequence (x, y^k) on all three axes.  Image and video tokens
