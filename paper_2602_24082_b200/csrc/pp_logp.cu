@@ -411,7 +411,7 @@ token_logp_kernel(LogpArgs p, int lg_parts, int rows, float* logp, float2* stats
     return;
   }
   // a warp looks over a row, then the block takes those that predict something
-  const long long mine = r + (long long)warp * gridDim.x;   // (of neighbours mostly all predict something or none does)
+  const long long mine = r + (long long)warp * gridDim.x;   // (of neighbours mostly all predict something or none)
   if (warp < rows) {
     Predicts u;
     u.n = 0;
@@ -578,12 +578,12 @@ LogpArgs logp_args(const pp_plan* plan, const void* logits, long long row_stride
 //    but 7 KB, T 450 6.4 (4 warps 4.2).  It has two vectors of a row up to 4 KB on their way and 12 blocks on
 //    an SM, else four and 8: 2.5 KB 17.2 and 20.5, 16 KB 22.4 and 17.9.  (Backward, 10 blocks: 3 KB, T 61100 74, with 8 78.)
 //  - 4 warps up to 32 KB, 8 beyond: 16 KB 22 and 33; 100 KB, T 990 backward 44 and 37.
-//  - forward, blocks that share a long row, where rows are few: 247 KB, T 242 17 (one), 12 (two), 9 (four); T 1020
-//    16 and 19, since the clusters of the rows that predict nothing have to be started too.
+//  - forward, blocks that share a long row, where rows are few: 247 KB, T 242 14 (one), 10 (two), 8.8 (four); 124 KB, T 128
+//    7.5 and 6.7; but T 1020 16 and 18: clusters start slowly, those of rows that predict nothing too.
 //  - backward, parts of 64 to 112 KB: 257 KB, T 9241 573 (one), 567 (two), 555 (four); smaller parts where
 //    rows are few: 557 KB, T 165 47 (one), 36 (two), 29 (four).
-//  - forward, rows that a block looks over: about one of them predicts something, and there are at most sixteen waves of blocks:
-//    257 KB, T 65536 of which one in nine 384 (one), 317 (eight), one in three 351 and 264; T 20000, one in
+//  - forward, rows that a block looks over: about one of them predicts something, and there are at most sixteen waves
+//    of blocks: 257 KB, T 65536 of which one in nine 384 (one), 317 (eight), one in three 351 and 264; T 20000, one in
 //    nine 119 and 100; but T 9241, every other one 194 and 217 (four).
 struct RowShape {
   int warps, lg_parts, rows, unroll;
@@ -612,7 +612,8 @@ RowShape row_shape(const pp_plan* plan, size_t row_bytes, int num_sms, bool fwd)
   return s;
 }
 dim3 blocks_of(int T, RowShape s) {
-  return dim3(s.warps == 1 ? unsigned((T + 3ll) / 4) : s.rows > 1 ? unsigned((T + s.rows - 1ll) / s.rows) : unsigned(T) << s.lg_parts);
+  const int rows = s.warps == 1 ? 4 : s.rows;
+  return dim3(unsigned((T + rows - 1ll) / rows) << s.lg_parts);
 }
 dim3 threads_of(RowShape s) { return dim3(s.warps == 1 ? 128 : s.warps * 32); }
 
