@@ -486,8 +486,9 @@ token_logp_bwd_kernel(LogpArgs p, LogpBwdArgs b, int lg_parts) {
     for (int at = sp.v0 + tid; at < sp.v1; at += kThreads) dst[at] = make_uint4(0, 0, 0, 0);
     return;
   }
-  // p_v = 2^(c x_v - K) 2^-f with K + f = (m + l) log2(e), K whole: 2^-f goes into the row's factor
-  const double lse2 = (double(st.x) + double(st.y)) * kLog2e;
+  // p_v = 2^(c x_v - K) 2^-f with K + f = c m + l log2(e) (m as it was before the temperature, c as it is in fp32),
+  // K whole: 2^-f goes into the row's factor
+  const double lse2 = double(st.x) * (double(p.temperature) * double(p.c)) + double(st.y) * kLog2e;
   const double whole = rint(lse2);
   const bool far = !(fabs(lse2) < double(kFar));
   const float scale = -float(total) / p.temperature;

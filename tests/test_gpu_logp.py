@@ -274,6 +274,26 @@ def test_rows_that_rise_fall_and_jump(V):
     _check_bwd(rows, logits, ids, g, 1.0, d, "fp32")
 
 
+@pytest.mark.parametrize("V", [300, 20000, 60000])
+@pytest.mark.parametrize("offset", [-4096.0, 30000.0])
+def test_an_offset_of_all_logits_costs_nothing(V, offset):
+    """Logits on a grid of 2^-8, which stay what they are with the offset: everything is relative to the row's maximum, so
+    the bounds are those of logits around zero, without the term for the exponent's size."""
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(2, (12, 9, 1))]]
+    logits, ids, _ = _inputs(rows, V, torch.float32, 3)
+    logits.copy_((logits * 256).round() / 256)
+    plan = _plan(rows)
+    g = torch.randn(len(ids), generator=torch.Generator().manual_seed(5)).cuda()
+    moved = logits + offset
+    assert torch.equal(moved - offset, logits)
+    logp, stats = B.pp_token_logp(plan, moved, ids)
+    d = B.pp_token_logp_bwd(plan, moved, ids, logp, stats, g)
+    stats[:, 0] -= offset * (stats[:, 0] != 0)
+    _check_fwd(rows, logits, ids, 1.0, logp, stats)
+    _check_bwd(rows, logits, ids, g, 1.0, d, "fp32")
+
+
 @pytest.mark.parametrize("V", [50, 5000, 70000])
 def test_the_same_id_of_several_responses_and_gradients_that_cancel(V):
     from paper_2602_24082_b200 import binding as B
