@@ -445,6 +445,7 @@ int pp_rope_qk_axes(const pp_plan* plan, const void* q, int64_t q_stride, const 
   if (q_stride < qd || q_out_stride < qd || k_stride < kd || k_out_stride < kd) return PP_ERR_INVALID_ARG;
   if (q_out == q && q_out_stride != q_stride) return PP_ERR_INVALID_ARG;
   if (k_out == k && k_out_stride != k_stride) return PP_ERR_INVALID_ARG;
+  if (q_out == k_out || q_out == k || k_out == q) return PP_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) ||
       ((q_stride | k_stride | q_out_stride | k_out_stride) & 7))
     return PP_ERR_ALIGNMENT;

@@ -84,3 +84,7 @@ def test_axes(lib, plan):
         args = list(good)
         args[i], args[j] = args[i - 4], args[j] + 8
         assert lib.pp_rope_qk_axes(*args) == -1
+    for i, other in ((5, 7), (7, 5), (5, 3), (7, 1)):     # one tensor's output on the other tensor
+        args = list(good)
+        args[i] = args[other]
+        assert lib.pp_rope_qk_axes(*args) == -1, (i, other)

@@ -402,6 +402,26 @@ def test_streams_graphs_and_repeats(V):
     assert not torch.equal(held[0], want[0])
 
 
+def test_given_outputs():
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(3, (4, 2))]]
+    logits, ids, _ = _inputs(rows, 1000, torch.float16, 1)
+    plan = _plan(rows)
+    logp, stats = B.pp_token_logp(plan, logits, ids)
+    a, b = torch.full((9,), 5.0, device="cuda"), torch.full((9, 2), 5.0, device="cuda")
+    for kw in (dict(token_logp=a), dict(row_stats=b), dict(token_logp=a, row_stats=b)):
+        a.fill_(5), b.fill_(5)
+        got = B.pp_token_logp(plan, logits, ids, **kw)
+        assert torch.equal(got[0], logp) and torch.equal(got[1], stats)
+        assert got[0] is kw.get("token_logp", got[0]) and got[1] is kw.get("row_stats", got[1])
+    for bad in (dict(token_logp=a[:-1]), dict(token_logp=a.half()), dict(row_stats=b.T), dict(row_stats=b.cpu())):
+        with pytest.raises(ValueError):
+            B.pp_token_logp(plan, logits, ids, **bad)
+    # what the call returns lies side by side in one allocation: writing to one leaves the others as they are
+    logp.fill_(3)
+    assert torch.equal(stats, b)
+
+
 def test_refusals():
     from paper_2602_24082_b200 import binding as B
     rows = [[(3, (4, 2))]]
