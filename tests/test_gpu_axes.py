@@ -68,6 +68,18 @@ def test_more_spans_in_a_group_than_a_block_holds_at_a_time():
     assert np.array_equal(pos.cpu().numpy(), A.position_ids(rows, starts, grids))
 
 
+def test_more_segments_and_spans_than_a_block_holds():
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(3, (2, 1)), (5, (7,))]] * 800
+    starts = [a + 1 for a, n, _, _, seg in W.Workload("s", rows, 1, 1, 64, seed=0).segments() if n in (3, 5, 7)]
+    grids = [[(1, 1, 2), (2, 1, 1), (1, 2, 1)][i % 3] for i in range(len(starts))]
+    assert len(starts) == 2400
+    plan = B.plan_for(W.Workload("axes", rows, 2, 1, 64, seed=0))
+    pos, status = B.pp_position_ids_axes(plan, _i32(starts), _i32(grids))
+    assert status.tolist() == [0, 0]
+    assert np.array_equal(pos.cpu().numpy(), A.position_ids(rows, starts, grids))
+
+
 @pytest.mark.parametrize("starts,grids,first", [
     ([2, 20], [(1, 2, 2), (1, 0, 3)], 1),                      # an empty side
     ([2, 20], [(1, -2, 2), (1, 1, 3)], 0),

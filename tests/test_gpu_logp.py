@@ -164,10 +164,10 @@ def test_parity_of_mostly_prompts(V, kind):
         _check_bwd(rows, safe, ids, g, 1.0, d, kind)
 
 
-@pytest.mark.parametrize("V", [257, 3000])
-def test_parity_of_many_short_rows(V):
+@pytest.mark.parametrize("V,rows", [(257, [[(2, (30, 31)), (40, (1, 2, 3))]] * 48), (3000, [[(2, (30, 31)), (40, (1, 2, 3))]] * 48),
+                                    (31, [[(2, (3, 1)), (1, (1,))]] * 1100)], ids=["257", "3000", "segments"])
+def test_parity_of_many_short_rows(V, rows):
     from paper_2602_24082_b200 import binding as B
-    rows = [[(2, (30, 31)), (40, (1, 2, 3))]] * 48
     logits, ids, _ = _inputs(rows, V, torch.bfloat16, 9)
     assert len(ids) > 32 * 148
     plan = _plan(rows)

@@ -28,6 +28,7 @@ CASES = {
     "parts8": [[(5000, (4097, 6000, 4100))]],
     "long": [[(9, (9000, 8191))], [(12000, (7000,))]],
     "many": [[(3, (40, 2)), (1, (1,) * 33)]] * 150,
+    "groups": [[(2, (3, 1)), (1, (1,))]] * 1100,
 }
 
 
