@@ -231,7 +231,8 @@ int pp_preference_loss(const pp_plan* plan, const float* token_logp, const float
  * need only a plan for the same descriptors, are one kernel on `stream`, and take DEVICE
  * pointers; results do not depend on the order in which blocks run.  They leave the plan as it is: calls on one
  * plan may overlap with each other and with the attention.  With a plan that the device has refused
- * (pp_plan_status) they write nothing.
+ * (pp_plan_status) they write nothing.  More than 2^31 - 2^16 tokens, or a vocabulary beyond 2^30, are
+ * PP_ERR_UNSUPPORTED.
  *
  * Position ids with a time, a height and a width axis (the paper trains on image prompts, Sec. 4).  A
  * token of text has the running number n of its unpacked sequence (x, y^k) on all three axes.  Image and video tokens
@@ -239,7 +240,7 @@ int pp_preference_loss(const pp_plan* plan, const float* token_logp, const float
  * span_start[i] on, frame by frame and row by row; if it starts at number n, its tokens are at
  * (n + frame, n + row, n + column) and what follows goes on at n + max(f, h, w).  Every response goes on
  * where its prompt ends.
- *   in : span_start [num_spans] ascending, span_grid [num_spans][3] (int32; may be NULL without spans).  A span lies
+ *   in : span_start [num_spans <= T] ascending, span_grid [num_spans][3] (int32; may be NULL without spans).  A span lies
  *        inside one segment (a prompt or a response); spans do not overlap
  *   out: position_ids [3][T] (int32); status [2]: 0 = fine, 1 = a span breaks these rules, and status[1] = the
  *        first such span (the positions of its group's tokens are then undefined)

@@ -418,10 +418,15 @@ int pp_preference_loss(const pp_plan* plan, const float* token_logp, const float
   return PP_OK;
 }
 
+// Token indices of the calls around the attention are 32 bits, and are stepped past the last one by a block's width.
+static bool too_long(const pp_plan* plan) { return plan->prob.total_tokens > INT32_MAX - 65536; }
+
 int pp_position_ids_axes(const pp_plan* plan, int32_t num_spans, const int32_t* span_start, const int32_t* span_grid,
                          int32_t* position_ids, int32_t* status, pp_stream_t stream) {
   g_last_launches = 0;
   if (!plan || !position_ids || !status || num_spans < 0) return PP_ERR_INVALID_ARG;
+  if (num_spans > plan->prob.total_tokens) return PP_ERR_INVALID_ARG;   // (they cannot all be one after the other)
+  if (too_long(plan)) return PP_ERR_UNSUPPORTED;
   if (num_spans && (!span_start || !span_grid)) return PP_ERR_INVALID_ARG;
   if (pp::launch_position_ids_axes(plan, num_spans, span_start, span_grid, position_ids, status,
                                    reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess)
@@ -439,6 +444,7 @@ int pp_rope_qk_axes(const pp_plan* plan, const void* q, int64_t q_stride, const 
   if (num_axes < 1 || num_axes > 4) return PP_ERR_INVALID_ARG;
   if (!(rope_base > 1.f) || rope_base > 1e12f) return PP_ERR_INVALID_ARG;
   const pp_problem& p = plan->prob;
+  if (too_long(plan)) return PP_ERR_UNSUPPORTED;
   for (int i = 0; i < p.head_dim / 2; ++i)
     if (axis_of_freq[i] >= num_axes) return PP_ERR_INVALID_ARG;
   const int64_t qd = int64_t(p.num_q_heads) * p.head_dim, kd = int64_t(p.num_kv_heads) * p.head_dim;
@@ -460,7 +466,7 @@ int pp_rope_qk_axes(const pp_plan* plan, const void* q, int64_t q_stride, const 
 static int check_logits(const pp_plan* plan, const void* logits, int32_t type, int64_t row_stride, int32_t vocab,
                         const void* token_ids, float temperature) {
   if (!plan || !logits || !token_ids || vocab < 1 || row_stride < vocab) return PP_ERR_INVALID_ARG;
-  if (type < PP_BF16 || type > PP_FP32) return PP_ERR_UNSUPPORTED;
+  if (type < PP_BF16 || type > PP_FP32 || vocab > 1 << 30 || too_long(plan)) return PP_ERR_UNSUPPORTED;
   if (!(temperature >= 1e-4f) || temperature > 1e4f) return PP_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(logits) & (type == PP_FP32 ? 3 : 1)) return PP_ERR_ALIGNMENT;
   return PP_OK;
@@ -509,6 +515,7 @@ int pp_policy_loss(const pp_plan* plan, const pp_policy* policy, const float* to
   if (!(o.clip_low >= 0) || o.clip_low > 1 || !(o.clip_high >= 0) || o.clip_high > 1e30) return PP_ERR_INVALID_ARG;
   if (!(o.kl_coef >= 0) || o.kl_coef > 1e30 || !(o.scale >= -1e30) || o.scale > 1e30) return PP_ERR_INVALID_ARG;
   if (!(o.eps > 0) || o.eps > 1e30) return PP_ERR_INVALID_ARG;
+  if (too_long(plan)) return PP_ERR_UNSUPPORTED;
   if (pp::launch_policy_loss(plan, o, token_logp, old_token_logp, ref_token_logp, reward, token_mask, advantage,
                              resp_loss, resp_kl, resp_clipped, d_token_logp,
                              reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess)

@@ -88,3 +88,19 @@ def test_axes(lib, plan):
         args = list(good)
         args[i] = args[other]
         assert lib.pp_rope_qk_axes(*args) == -1, (i, other)
+
+
+def test_sizes_beyond_32_bit_indices(lib, plan):
+    w = W.Workload("e", [[(5, (2, 4))]], 4, 2, 64, seed=0)
+    p, keep = B.make_problem(w.descriptors(), 4, 2, 64, 2 ** 31 - 1000)
+    long = ctypes.create_string_buffer(4096)
+    ctypes.memmove(long, ctypes.byref(p), ctypes.sizeof(p))
+    axis = ctypes.create_string_buffer(bytes(32), 32)
+    policy = ctypes.byref(Policy(2, 0, 0.2, 0.2, 0.0, 1.0, 1e-6))
+    assert lib.pp_token_logp(long, A, 0, 100, 100, A, 0, 1.0, A, A, None) == -2
+    assert lib.pp_token_logp(plan, A, 0, 2 ** 31, 2 ** 30 + 1, A, 0, 1.0, A, A, None) == -2
+    assert lib.pp_token_logp_bwd(long, A, 0, 100, 100, A, 0, 1.0, A, A, A, 2 * A, 100, None) == -2
+    assert lib.pp_policy_loss(long, policy, A, None, None, A, None, None, A, A, A, None, None) == -2
+    assert lib.pp_rope_qk_axes(long, A, 256, 2 * A, 128, 3 * A, 256, 4 * A, 128, A, 3, axis, 10000.0, 0, None) == -2
+    assert lib.pp_position_ids_axes(long, 0, None, None, A, A, None) == -2
+    assert lib.pp_position_ids_axes(plan, 12, A, A, A, A, None) == -1      # more spans than tokens
