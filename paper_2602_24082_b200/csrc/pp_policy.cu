@@ -129,7 +129,8 @@ __global__ void __launch_bounds__(kThreads) policy_loss_kernel(PolicyArgs p, int
       for (int j = lane + 32; j < n; j += 32) sum += p.reward[x0 + j];
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      const double mean = sum * inv_n;
+      // the quotient as a division rounds it: equal rewards have to have themselves for mean, and no advantage
+      const double q = sum * inv_n, mean = fma(fma(-q, double(n), sum), inv_n, q);
       A -= mean;
       if (p.o.advantage_mode == PP_ADVANTAGE_NORMALIZED) {
         double sq = lane < n ? (mine - mean) * (mine - mean) : 0.0;

@@ -127,6 +127,21 @@ def test_borders_and_extremes():
         assert float(cut[0]) == np.float32((~keep[:7]).sum() / 7)
 
 
+@pytest.mark.parametrize("mode", ["centered", "normalized"])
+def test_equal_rewards_have_no_advantage(mode):
+    """Their mean is the reward itself, exactly, whatever it and their number are."""
+    from paper_2602_24082_b200 import binding as B
+    sizes = [1, 2, 3, 5, 6, 7, 11, 33, 49, 100, 641]
+    rows = [[(2, (1,) * n)] for n in sizes]
+    plan = B.plan_for(W.Workload("policy", rows, 2, 1, 64, seed=0))
+    rng = np.random.default_rng(0)
+    lp = _cuda(-rng.gamma(1.0, 1.5, sum(sizes) + 2 * len(sizes)).astype(np.float32))
+    for _ in range(20):
+        r = np.repeat(rng.normal(size=len(sizes)).astype(np.float32), sizes)
+        loss, _, _, adv, grad = B.pp_policy_loss(plan, lp, None, None, _cuda(r), advantage=mode)
+        assert not adv.any() and not loss.any() and not grad.any()
+
+
 def test_gradient_against_differences():
     """fp32 losses of size 1 moved by 2^-9 along a direction: 2 u / h of rounding and the curvature's h^2.  Ratios
     stay clear of the borders, where there is no slope."""
