@@ -218,14 +218,19 @@ cudaError_t launch_policy_loss(const pp_plan* plan, const pp_policy& o, const fl
   p.kl = kl;
   p.clipped = clipped;
   p.d_logp = d_logp;
-  // a team's threads take about two tokens of a mean segment each
-  const int mean = plan->prob.total_tokens / plan->nseg;
-  const int N = p.N;
-  if (mean <= 64) return launch_kernel(true, policy_loss_kernel<32>, dim3((N + 7) / 8), dim3(kThreads), 0, stream, p, 1);
-  if (mean <= 128) return launch_kernel(true, policy_loss_kernel<64>, dim3((N + 3) / 4), dim3(kThreads), 0, stream, p, 1);
-  if (mean <= 256) return launch_kernel(true, policy_loss_kernel<128>, dim3((N + 1) / 2), dim3(kThreads), 0, stream, p, 1);
-  int parts = 1;
-  while (parts < kMaxParts && mean > kThreads * parts && (long long)N * 2 * parts <= 4ll * dev->num_sms) parts *= 2;
+  // A team has up to four threads for a token of a mean segment, while all of them fit the chip, and a
+  // cluster of blocks where segments are long.  us, by tokens of a mean segment and responses: 18, 1880 5.1 (32
+  // threads), 5.2 (64), 12.5 (256); 94, 376 8.1, 6.0, 5.0; 100, 20 7.7, 5.8, 4.3; 307, 104 19, 11, 6.2, blocks by twos 6.8, by
+  // fours 6.4; 809, 72 8.9 (256), 8.5 (two blocks), 7.1 (four), 8.4 (eight); 2427, 18 16, 13, 9.5, 7.8.
+  const long long N = p.N, mean = plan->prob.total_tokens / plan->nseg, most = 2048ll * dev->num_sms;
+  if (32 * 2 > 4 * mean || N * 64 > most)
+    return launch_kernel(true, policy_loss_kernel<32>, dim3(unsigned((N + 7) / 8)), dim3(kThreads), 0, stream, p, 1);
+  if (64 * 2 > 4 * mean || N * 128 > most)
+    return launch_kernel(true, policy_loss_kernel<64>, dim3(unsigned((N + 3) / 4)), dim3(kThreads), 0, stream, p, 1);
+  if (128 * 2 > 4 * mean || N * 256 > most)
+    return launch_kernel(true, policy_loss_kernel<128>, dim3(unsigned((N + 1) / 2)), dim3(kThreads), 0, stream, p, 1);
+  int parts = mean > 1536 ? 8 : mean > 400 ? 4 : 1;
+  if (N * parts > 4ll * dev->num_sms) parts = N * 4 > 4ll * dev->num_sms ? 1 : 4;
   return launch_clusters(parts, policy_loss_kernel<kThreads>, dim3(unsigned(N) * parts), dim3(kThreads), 0, stream, p,
                          parts);
 }

@@ -126,7 +126,7 @@ SECTIONS = {64: [(8, 12, 12), (32,), (1, 30, 1), (8, 8, 8, 8)], 96: [(12, 18, 18
             128: [(16, 24, 24), (64,), (20, 4, 40), (16, 16, 16, 16)]}
 
 
-@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (7, 1), (32, 8), (14, 2), (64, 8)])
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (7, 1), (32, 8), (14, 2), (64, 8), (140, 20)])
 @pytest.mark.parametrize("D", [64, 96, 128])
 @pytest.mark.parametrize("inverse", [False, True])
 def test_rope_parity(Hq, Hkv, D, inverse):

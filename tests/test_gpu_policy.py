@@ -29,6 +29,8 @@ CASES = {
     "long": [[(9, (9000, 8191))], [(12000, (7000,))]],
     "many": [[(3, (40, 2)), (1, (1,) * 33)]] * 150,
     "groups": [[(2, (3, 1)), (1, (1,))]] * 1100,
+    "mean20": [[(20, (25, 15, 21)), (9, (40,))]] * 9,
+    "mean40": [[(40, (45, 30, 51)), (9, (80,))]] * 9,
 }
 
 
