@@ -392,7 +392,7 @@ __device__ __forceinline__ void token_logp_row(const LogpArgs& p, const Predicts
   }
 }
 
-// `rows`: what a block of more than one warp looks over at once (with lg_parts == 0).
+// `rows`: what a block of eight warps looks over at once (with lg_parts == 0).
 template <typename X, int kWarps, int kUnroll>
 __global__ void __launch_bounds__(block_threads<kWarps>(), blocks_per_sm<kWarps, kUnroll>())
 token_logp_kernel(LogpArgs p, int lg_parts, int rows, float* logp, float2* stats) {
@@ -403,7 +403,7 @@ token_logp_kernel(LogpArgs p, int lg_parts, int rows, float* logp, float2* stats
   if (kWarps == 1 && r >= p.T) return;
   dependency_wait();
   bool fine;
-  if (kWarps == 1 || rows == 1) {
+  if (kWarps < 8 || rows == 1) {
     const Predicts u = predicts_of(p, r, fine);
     if (!fine || !row_used(p, u, part == 0 && (kWarps == 1 || warp == 0), logp, stats)) return;
     if (kWarps > 1 && lg_parts) cooperative_groups::this_cluster().barrier_arrive();
@@ -574,41 +574,56 @@ LogpArgs logp_args(const pp_plan* plan, const void* logits, long long row_stride
 }
 
 // How the rows are dealt out: warps of a row's team, blocks that share a row, rows that a block looks over,
-// vectors of a thread that are on their way at a time.  us on one B200, by bytes of a row and T rows:
-//  - a warp for a short row, where there are enough of them: 2.5 KB, T 37872 17 (4 warps 57); 16 KB, T 7867 18 (4 warps 22);
-//    but 7 KB, T 450 6.4 (4 warps 4.2).  It has two vectors of a row up to 4 KB on their way and 12 blocks on
-//    an SM, else four and 8: 2.5 KB 17.2 and 20.5, 16 KB 22.4 and 17.9.  (Backward, 10 blocks: 3 KB, T 61100 74, with 8 78.)
-//  - 4 warps up to 32 KB, 8 beyond: 16 KB 22 and 33; 100 KB, T 990 backward 44 and 37.
-//  - forward, blocks that share a long row, where rows are few: 247 KB, T 242 14 (one), 10 (two), 8.8 (four); 124 KB, T 128
-//    7.5 and 6.7; but T 1020 16 and 18: clusters start slowly, those of rows that predict nothing too.
-//  - backward, parts of 64 to 112 KB: 257 KB, T 9241 573 (one), 567 (two), 555 (four); smaller parts where
-//    rows are few: 557 KB, T 165 47 (one), 36 (two), 29 (four).
-//  - forward, rows that a block looks over: about one of them predicts something, and there are at most sixteen waves
-//    of blocks: 257 KB, T 65536 of which one in nine 384 (one), 317 (eight), one in three 351 and 264; T 20000, one in
-//    nine 119 and 100; but T 9241, every other one 194 and 217 (four).
+// vectors of a thread that are on their way at a time.  us on one B200, bf16, by T rows of V columns, half of which predict
+// something where it is not said otherwise:
+//  - a warp where there are rows enough: V 600, T 60000 26 (4 warps 106); 12000, 20000 45 and 56; 25000, 20000 85 and 91;
+//    but 25000, 6000 41 and 32; 3001, 700 5.1 and 4.3.  Two vectors at a time of many short rows: 600, 60000 26 (four:
+//    30), but 1500, 6000 7.2 and 6.7, 12000, 20000 49 and 45.
+//  - 4 warps, then 8: 25000, 6000 32 (8 warps 41); 60000, 6000 61 and 64, with one row in nine 26 and 27; 25000, 700 8.8 and
+//    8.5; fp32, 50257, 3001 57 and 55.  Backward 12000, 2000 16 and 17; 25000, 6000 76 and 77, with one in nine 61 and 57.
+//  - forward, blocks that share a long row, where rows are few: 140000, 60 16 (8 warps), 10 (two blocks), 7.9 (four);
+//    60000, 60 7.0, 6.2 and 6.0; 140000, 700 27, 24 and 28; but 60000, 700 14.5, 15 and 19: clusters start slowly, those of
+//    rows that predict nothing too.
+//  - backward, parts of 64 to 112 KB: 128256, 9241 573 (one), 567 (two), 555 (four); smaller ones where rows are
+//    few: 140000, 60 35 (one), 13 (four), 8.1 (eight); 12000, 200 5.2, 4.5 (two) and 4.3 (four).
+//  - forward, rows that a block looks over, with sixteen waves of blocks or more: 128256, 65536, one in nine 378 (one),
+//    306 (eight); 20000, one in nine 116 and 97; but 140000, 2000, half 49 (one) and 55 (two).
 struct RowShape {
   int warps, lg_parts, rows, unroll;
 };
 RowShape row_shape(const pp_plan* plan, size_t row_bytes, int num_sms, bool fwd) {
-  const long long T = plan->prob.total_tokens;
+  const long long T = plan->prob.total_tokens, sms = num_sms;
   RowShape s{8, 0, 1, 4};
-  if (row_bytes <= (T > 32ll * num_sms ? 16384 : T > 8ll * num_sms ? 4096 : 0)) {
+  const size_t one_warp = fwd ? (T > 64 * sms ? 65536 : T > 32 * sms ? 16384 : T > 8 * sms ? 8192 : 0)
+                              : (T > 32 * sms ? 16384 : T > 8 * sms ? 2048 : 0);
+  if (row_bytes <= one_warp) {
     s.warps = 1;
-    if (row_bytes <= 4096 && fwd) s.unroll = 2;
+    if (row_bytes <= 8192 && T > 64 * sms) s.unroll = 2;
     return s;
   }
-  if (row_bytes <= 32768) s.warps = 4;
   if (fwd) {
-    if (s.warps == 8)
-      while (s.lg_parts < kMaxLgParts && (T << (s.lg_parts + 1)) <= 7ll * num_sms && row_bytes >> (s.lg_parts + 1) >= 49152)
-        ++s.lg_parts;
-    // rows that predict something: all but the last of a response, and one of a prompt
-    const long long used = plan->resp_tokens - plan->prob.num_responses + plan->prob.num_groups;
-    const long long rows = std::max(plan->resp_tokens ? T / std::max(used, 1ll) : 0, T / (16ll * (32 / s.warps) * num_sms));
-    if (T > 7ll * num_sms) s.rows = int(std::max(1ll, std::min(rows, (long long)s.warps)));
-  } else if (s.warps == 8) {
-    auto few = [&](int lg) { return (T << (lg + 1)) <= 4ll * num_sms && row_bytes >> (lg + 1) >= 16384; };
-    while (s.lg_parts < kMaxLgParts && (row_bytes >> s.lg_parts > 114688 || few(s.lg_parts))) ++s.lg_parts;
+    if (row_bytes <= (T > 32 * sms ? 131072 : T > 8 * sms ? 65536 : 32768)) {
+      s.warps = 4;
+    } else {
+      auto share = [&](int lg) {
+        const size_t part = row_bytes >> lg;
+        return (T << lg) <= (part >= 122880 ? 10 : part >= 49152 ? 7 : part >= 14336 && row_bytes >= 98304 ? 3 : 0) * sms;
+      };
+      while (s.lg_parts < kMaxLgParts && share(s.lg_parts + 1)) ++s.lg_parts;
+      // rows that predict something: all but the last of a response, and one of a prompt
+      const long long used = plan->resp_tokens - plan->prob.num_responses + plan->prob.num_groups, waves = T / (4 * sms);
+      if (waves >= 16) s.rows = int(std::min(8ll, std::max(waves / 16, plan->resp_tokens ? T / std::max(used, 1ll) : 1)));
+    }
+  } else {
+    if (row_bytes <= (T > 8 * sms ? 32768 : 2 * T > 3 * sms ? 8192 : 0)) {
+      s.warps = 4;
+    } else {
+      auto share = [&](int lg) {
+        const size_t part = row_bytes >> lg;
+        return row_bytes >> (lg - 1) > 114688 || (T << lg) <= (part >= 8192 ? 6 : part >= 2048 ? 3 : 0) * sms;
+      };
+      while (s.lg_parts < kMaxLgParts && share(s.lg_parts + 1)) ++s.lg_parts;
+    }
   }
   return s;
 }

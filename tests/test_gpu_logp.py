@@ -146,7 +146,7 @@ def test_parity_of_large_vocabularies(tokens, V, kind):
 @pytest.mark.parametrize("kind", ["bf16", "fp32"])
 @pytest.mark.parametrize("V", [600, 9001, 20000])
 def test_parity_of_mostly_prompts(V, kind):
-    """Blocks that look over several rows at once, of which few predict something."""
+    """Few rows that predict something; the others are not read."""
     from paper_2602_24082_b200 import binding as B
     rows = [[(1200, (40, 30, 9))], [(90, (3,)), (1, (1, 2))]]
     logits, ids, _ = _inputs(rows, V, TYPES[kind][0], 7)
@@ -178,7 +178,7 @@ def test_parity_of_many_short_rows(V, rows):
     _check_bwd(rows, logits, ids, g, 1.0, d, "bf16")
 
 
-@pytest.mark.parametrize("T,V", [(20000, 17000), (40000, 5001)])
+@pytest.mark.parametrize("T,V", [(20000, 17000), (40000, 5001), (9600, 66000), (12345, 66001)])
 def test_the_way_rows_are_dealt_out_does_not_change_them(T, V):
     """A plan from host arrays knows how many tokens the responses hold, one from device arrays does not: their
     blocks look over other numbers of rows."""
