@@ -231,6 +231,22 @@ __device__ __forceinline__ Running join_lanes(Running a) {
   return a;
 }
 
+// the maximum of a row's threads; after it, all of them have come here
+template <int kWarps>
+__device__ __forceinline__ float row_max(float m) {
+  int top = __reduce_max_sync(0xffffffffu, ordered(m));
+  if constexpr (kWarps > 1) {
+    __shared__ int warp_top[kWarps];
+    if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) top = max(top, warp_top[w]);
+  } else {
+    __syncwarp();
+  }
+  return from_ordered(top);
+}
+
 struct JoinSpace {
   Running warp[8], part[8];
 };
@@ -478,7 +494,7 @@ token_logp_bwd_kernel(LogpArgs p, LogpBwdArgs b, int lg_parts) {
 
   const X* row = static_cast<const X*>(p.logits) + (long long)r * p.row_stride;
   X* out = static_cast<X*>(b.d_logits) + (long long)r * b.d_stride;
-  const Span sp = span_of<128>(out, p.V, part, lg_parts);
+  Span sp = span_of<128>(out, p.V, part, lg_parts);
   uint4* dst = reinterpret_cast<uint4*>(out + sp.head);
   if (!any) {
     for (int i = tid; i < sp.edge + sp.tail; i += kThreads)
@@ -491,24 +507,25 @@ token_logp_bwd_kernel(LogpArgs p, LogpBwdArgs b, int lg_parts) {
   const double lse2 = double(st.x) * (double(p.temperature) * double(p.c)) + double(st.y) * kLog2e;
   const double whole = rint(lse2);
   const bool far = !(fabs(lse2) < double(kFar));
-  const float scale = -float(total) / p.temperature;
-  const float coef = far ? scale : scale * exp2f(float(whole - lse2));
-  const float K = float(whole), c = p.c;
-  auto one = [&](float x) {
-    return far ? scale * expf(x / p.temperature - st.x - st.y) : coef * ex2(fmaf(x, c, -K));
-  };
-  for (int i = tid; i < sp.edge + sp.tail; i += kThreads) {
-    const int e = i < sp.edge ? i : sp.tail0 + i - sp.edge;
-    Row<X>::store(out + e, one(Row<X>::one(row[e])));
-  }
-  if (kVec && !far) {
-    const uint4* vec = reinterpret_cast<const uint4*>(row + sp.head);
+  const float scale = -float(total) / p.temperature, c = p.c;
+  const uint4* vec = reinterpret_cast<const uint4*>(row + sp.head);
+  // the gradient as `one` has it of an element
+  auto write = [&](auto one) {
+    for (int i = tid; i < sp.edge + sp.tail; i += kThreads) {
+      const int e = i < sp.edge ? i : sp.tail0 + i - sp.edge;
+      Row<X>::store(out + e, one(Row<X>::one(row[e])));
+    }
+    if (!kVec) {
+      for (int e = sp.head + sp.v0 * kN + tid; e < sp.head + sp.v1 * kN; e += kThreads)
+        Row<X>::store(out + e, one(Row<X>::one(row[e])));
+      return;
+    }
     auto take = [&](uint4 v) {
       uint32_t w[4];
       int i = 0;
       for_pairs<X>(v, [&](float x, float y) {
-        x = ex2(fmaf(x, c, -K)) * coef;
-        y = ex2(fmaf(y, c, -K)) * coef;
+        x = one(x);
+        y = one(y);
         if constexpr (kN == 8) {
           w[i++] = Row<X>::word(x, y);
         } else {
@@ -527,9 +544,22 @@ token_logp_bwd_kernel(LogpArgs p, LogpBwdArgs b, int lg_parts) {
       for (int i = 0; i < kUnroll; ++i)
         if (at + i * kThreads < sp.v1) dst[at + i * kThreads] = take(v[i]);
     }
+  };
+  if (!far) {
+    const float coef = scale * exp2f(float(whole - lse2)), K = float(whole);
+    write([&](float x) { return ex2(fmaf(x, c, -K)) * coef; });
   } else {
-    for (int e = sp.head + sp.v0 * kN + tid; e < sp.head + sp.v1 * kN; e += kThreads)
-      Row<X>::store(out + e, one(Row<X>::one(row[e])));
+    // Beyond +-2^19 a power relative to a reference loses its digits, and m / temperature itself may have
+    // passed fp32's range, so that row_stats do not tell m: it is read again, and everything is relative to
+    // it as in the forward.  By one block for the whole row: in place, other blocks would find theirs overwritten.
+    if (part > 0) return;
+    lg_parts = 0;
+    sp = span_of<128>(out, p.V, 0, 0);
+    float m = -INFINITY;   // (with a NaN, or no finite maximum, l is one)
+    for (int e = tid; e < p.V; e += kThreads) m = fmaxf(m, Row<X>::one(row[e]));
+    m = row_max<kWarps>(m);
+    const float coef = scale * expf(-st.y);
+    write([&](float x) { return ex2((x - m) * c) * coef; });
   }
   // the tokens' own columns, from their log-probabilities: 1 - p without cancellation.  The same id may be
   // that of several responses: each writes the sum over all of them.

@@ -444,3 +444,52 @@ def test_refusals():
     for args in ((logp[:-1], stats, g), (logp, stats.T, g), (logp, stats, g.double()), (logp, stats, g.cpu())):
         with pytest.raises(ValueError):
             B.pp_token_logp_bwd(plan, logits, ids, *args)
+
+
+# A warp, 128 threads, 256 threads and several blocks take a row of the gradient.
+BACKWARD_SHAPES = [(100, [[(5, (700, 600))]]), (5000, [[(5, (700, 600))]]), (300, [[(2, (12, 9, 1))]]), (20000, [[(2, (12, 9, 1))]]),
+                   (140000, [[(2, (12, 9, 1))]])]
+BACKWARD_IDS = ["warp", "four_warps", "few", "two_blocks", "eight_blocks"]
+
+
+@pytest.mark.parametrize("V,rows", BACKWARD_SHAPES, ids=BACKWARD_IDS)
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("temperature", [0.7, 1.0, 1.3])
+def test_rows_far_from_zero_at_any_temperature(V, rows, kind, temperature):
+    """Rows at the ends of the type's range, whose maximum over the temperature may pass fp32's: log-probabilities and
+    gradients are those relative to the maximum (the bounds without the term for the exponent's size), in place too."""
+    from paper_2602_24082_b200 import binding as B
+    dtype, lowest = TYPES[kind][0], torch.finfo(TYPES[kind][0]).min
+    logits, ids, _ = _inputs(rows, V, dtype, 1)
+    x, n = logits, torch.arange(V, device="cuda")
+    first = rows[0][0][0]                      # the first response's rows
+    near = torch.tensor(lowest, device="cuda").to(dtype) * 0.75
+    x[first] = lowest
+    x[first + 1] = -lowest
+    x[first + 2] = torch.where(n % 3 == 1, near, x[first])          # all of them beyond 0.7 of the range
+    x[first + 3] = torch.where(n % 7 == 2, -near, x[first])
+    x[first + 4] = torch.where(n == V - 1, 2.5, lowest)
+    x[first + 5] = torch.where(n < V // 2, -torch.inf, near)
+    ids[first + 1: first + 7] = torch.tensor([0, 0, 1, 2, 0, V - 1]).cuda()
+    plan = _plan(rows)
+    logp, stats = B.pp_token_logp(plan, logits, ids, temperature)
+    # the same rows relative to their maximum, in 64 bits
+    safe = logits.double() - logits.double().amax(1, keepdim=True)
+    temp = float(np.float32(temperature))
+    want, st = P.token_logp(rows, _f64(safe), ids.cpu().numpy(), temp)
+    got = _f64(logp)
+    l = np.zeros(len(want))
+    for r, t in P.predictions(rows):
+        l[t] = st[r, 1]
+    tol = U * (600 + 8 * np.abs(l) + 8 * np.abs(want + l))
+    # (beyond fp32's largest number a log-probability is -inf)
+    assert (np.abs(got - want) <= tol)[np.abs(want) < 3e38].all()
+    assert (got[np.abs(want) > 3.5e38] == -np.inf).all()
+    assert np.isfinite(_f64(stats)[:, 1]).all()
+    g = torch.randn(len(ids), generator=torch.Generator().manual_seed(5)).cuda()
+    d = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g, temperature)
+    _check_bwd(rows, safe, ids, g, temperature, d, kind)
+    other = torch.full((len(ids), V + 3), 5.0, dtype=dtype, device="cuda")
+    B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g, temperature, d_logits=other[:, :V])
+    assert torch.equal(other[:, :V], d)
+    assert torch.equal(B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g, temperature, d_logits=logits), d)
