@@ -36,6 +36,7 @@ namespace pp {
 namespace {
 
 constexpr float kFar = 524288.f;   // |c m| up to which ceil(c m) is at most 1 above c m
+constexpr float kFarOther = 512.f; // the same in the gradient of fp32 logits at a temperature
 constexpr int kMostK = 1 << 20;
 constexpr float kSlack = 64.f;     // powers up to 2^64 are summed up: 2^95 with the longest row
 constexpr float kLn2 = 0.693147180559945309f;
@@ -61,6 +62,7 @@ template <> struct Row<__nv_bfloat16> {
   static constexpr uint32_t kLeast = 0xff80ff80u;   // -inf, twice
   static __device__ __forceinline__ float one(const __nv_bfloat16& x) { return __bfloat162float(x); }
   static __device__ __forceinline__ void store(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+  static __device__ __forceinline__ float round(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
   static __device__ __forceinline__ void pair(uint32_t w, float& a, float& b) {
     a = __uint_as_float(w << 16);
     b = __uint_as_float(w & 0xffff0000u);
@@ -81,6 +83,7 @@ template <> struct Row<__half> {
   static constexpr uint32_t kLeast = 0xfc00fc00u;
   static __device__ __forceinline__ float one(const __half& x) { return __half2float(x); }
   static __device__ __forceinline__ void store(__half* p, float x) { *p = __float2half_rn(x); }
+  static __device__ __forceinline__ float round(float x) { return __half2float(__float2half_rn(x)); }
   static __device__ __forceinline__ void pair(uint32_t w, float& a, float& b) {
     const float2 f = __half22float2(reinterpret_cast<const __half2&>(w));
     a = f.x;
@@ -503,10 +506,15 @@ token_logp_bwd_kernel(LogpArgs p, LogpBwdArgs b, int lg_parts) {
     return;
   }
   // p_v = 2^(c x_v - K) 2^-f with K + f = c m + l log2(e) (m as it was before the temperature, c as it is in fp32),
-  // K whole: 2^-f goes into the row's factor
-  const double lse2 = double(st.x) * (double(p.temperature) * double(p.c)) + double(st.y) * kLog2e;
+  // K whole: 2^-f goes into the row's factor.  row_stats hold m / temperature, rounded to fp32.  That times the temperature
+  // is within 2^-23 of m, which rounded to 16 bits is m itself, and m without a temperature.  Of other fp32
+  // rows all probabilities have a factor of up to 1 + 2^-24 |m| / temperature, so that they pass for far ones early.
+  double m_of = double(st.x) * double(p.temperature), near = kFar;
+  if constexpr (sizeof(X) == 2) m_of = Row<X>::round(float(m_of));
+  else if (p.temperature != 1.f) near = kFarOther;
+  const double lse2 = m_of * double(p.c) + double(st.y) * kLog2e;
   const double whole = rint(lse2);
-  const bool far = !(fabs(lse2) < double(kFar));
+  const bool far = !(fabs(lse2) < near);
   const float scale = -float(total) / p.temperature, c = p.c;
   const uint4* vec = reinterpret_cast<const uint4*>(row + sp.head);
   // the gradient as `one` has it of an element
@@ -549,9 +557,8 @@ token_logp_bwd_kernel(LogpArgs p, LogpBwdArgs b, int lg_parts) {
     const float coef = scale * exp2f(float(whole - lse2)), K = float(whole);
     write([&](float x) { return ex2(fmaf(x, c, -K)) * coef; });
   } else {
-    // Beyond +-2^19 a power relative to a reference loses its digits, and m / temperature itself may have
-    // passed fp32's range, so that row_stats do not tell m: it is read again, and everything is relative to
-    // it as in the forward.  By one block for the whole row: in place, other blocks would find theirs overwritten.
+    // Far from zero c x loses its digits, and m / temperature itself may have passed fp32's range, so that
+    // row_stats do not tell m: it is read again, and everything is relative to it as in the forward.  By one block for the whole row: in place, other blocks would find theirs overwritten.
     if (part > 0) return;
     lg_parts = 0;
     sp = span_of<128>(out, p.V, 0, 0);

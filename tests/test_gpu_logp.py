@@ -493,3 +493,38 @@ def test_rows_far_from_zero_at_any_temperature(V, rows, kind, temperature):
     B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g, temperature, d_logits=other[:, :V])
     assert torch.equal(other[:, :V], d)
     assert torch.equal(B.pp_token_logp_bwd(plan, logits, ids, logp, stats, g, temperature, d_logits=logits), d)
+
+
+@pytest.mark.parametrize("V,rows", BACKWARD_SHAPES, ids=BACKWARD_IDS)
+@pytest.mark.parametrize("kind,offset,grid", [("fp32", 200.0, 2.0 ** -12), ("fp32", -4096.0, 2.0 ** -8), ("fp32", 30000.0, 2.0 ** -8), ("fp32", 3e6, 0.25),
+                                              ("fp16", 800.0, 0.5), ("fp16", -30000.0, 16.0), ("bf16", -800.0, 4.0),
+                                              ("bf16", 196608.0, 1024.0), ("bf16", 3145728.0, 16384.0)])
+@pytest.mark.parametrize("temperature", [0.7, 1.3, 0.01])
+def test_an_offset_costs_nothing_at_a_temperature(V, rows, kind, offset, grid, temperature):
+    """Logits on the type's grid around an offset.  row_stats hold the maximum over the temperature, rounded to fp32: for
+    16-bit logits the maximum itself follows from it, fp32 rows far from zero are read again, so the bounds are those of logits
+    whose maximum is zero.  Of other fp32 rows the gradient has that rounding, u |m| / temperature, for a factor."""
+    from paper_2602_24082_b200 import binding as B
+    logits, ids, _ = _inputs(rows, V, torch.float32, 3)
+    base = (logits * max(1.0, temperature) * (1 if grid < 1 else grid / 2) / grid).round() * grid
+    moved = (base + offset).to(TYPES[kind][0])
+    assert torch.equal(moved.double() - offset, base.double())
+    safe = base.double() - base.double().amax(1, keepdim=True)
+    plan = _plan(rows)
+    logp, stats = B.pp_token_logp(plan, moved, ids, temperature)
+    g = torch.randn(len(ids), generator=torch.Generator().manual_seed(5)).cuda()
+    d = B.pp_token_logp_bwd(plan, moved, ids, logp, stats, g, temperature)
+    temp = float(np.float32(temperature))
+    want, st = P.token_logp(rows, _f64(safe), ids.cpu().numpy(), temp)
+    l = np.zeros(len(want))
+    for r, t in P.predictions(rows):
+        l[t] = st[r, 1]
+    assert (np.abs(_f64(logp) - want) <= U * (600 + 8 * np.abs(l) + 8 * np.abs(want + l))).all()
+    top = float(base.amax()) + abs(offset)
+    if kind == "fp32" and top / temp * 1.4427 < 512:
+        # (a factor 1 + e of the probabilities, e <= u |m| / temperature)
+        want, size = P.token_logp_bwd(rows, _f64(safe), ids.cpu().numpy(), _f64(g), temp)
+        assert (np.abs(_f64(d) - want) <= U * (700 + 8 * np.log2(V + 1) + 2 * top / temp) * size + 2.0 ** -120).all()
+    else:
+        _check_bwd(rows, safe, ids, g, temperature, d, kind)
+    assert torch.equal(B.pp_token_logp_bwd(plan, moved, ids, logp, stats, g, temperature, d_logits=moved), d)
