@@ -19,10 +19,11 @@
 // temperature, with a whole number K for reference: K is exact in fp32, so nothing of c x is
 // lost to the rounding of a reference (c m rounded would be off by 2^-24 |c m|, the same for the whole
 // row), and sums of different references are joined by exact powers of two.  K comes from a thread's first elements and
-// stays unless one is 2^64 times as large: a new reference with every new maximum was a branch that some lane of
+// stays unless one is 2^8 times as large: a new reference with every new maximum was a branch that some lane of
 // a warp took in nearly every step (with it, and a look at the row's end for every vector, 128 instead of 105 million
-// instructions; under the power limit of a long run, at 1.7 GHz, 219 us instead of 201 - 210).  A thread has four
-// 16-byte vectors on their way while it sums up four (without that 252 us).
+// instructions; under the power limit of a long run, at 1.7 GHz, 219 us instead of 210).  An exponent of up to 8 is rounded
+// to 2^-22; up to 64 it was 2^-19, which of a certain token's log-probability is the whole, and no faster (195
+// us and 210, both).  A thread has four 16-byte vectors on their way while it sums up four (without that 252 us).
 // Rows whose values are beyond +-2^19 (a mask of the type's lowest value over everything, say)
 // go through a second pass over exp(x - m).
 #include <cooperative_groups.h>
@@ -36,9 +37,9 @@ namespace pp {
 namespace {
 
 constexpr float kFar = 524288.f;   // |c m| up to which ceil(c m) is at most 1 above c m
-constexpr float kFarOther = 512.f; // the same in the gradient of fp32 logits at a temperature
+constexpr float kFarOther = 512.f;  // the same in the gradient of fp32 logits at a temperature
 constexpr int kMostK = 1 << 20;
-constexpr float kSlack = 64.f;     // powers up to 2^64 are summed up: 2^95 with the longest row
+constexpr float kSlack = 8.f;      // powers up to 2^8 are summed up: 2^38 with the longest row
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr double kLog2e = 1.4426950408889634074;
 

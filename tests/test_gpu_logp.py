@@ -528,3 +528,38 @@ def test_an_offset_costs_nothing_at_a_temperature(V, rows, kind, offset, grid, t
     else:
         _check_bwd(rows, safe, ids, g, temperature, d, kind)
     assert torch.equal(B.pp_token_logp_bwd(plan, moved, ids, logp, stats, g, temperature, d_logits=moved), d)
+
+
+@pytest.mark.parametrize("V", [600, 5000, 50257, 128256])
+@pytest.mark.parametrize("temperature", [1.0, 0.7])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_certain_tokens(V, temperature, kind):
+    """One column far above the others, in every part of the row.  log p = -log1p(sum of the others), to within u times
+      4    the power of that column (2^-22),
+      2.8  its exponent, at most 8 above the reference: half a step of 4 .. 8, 2^-22, times log 2,
+      1.5  log S (one step of up to log 2) and what is left of the maximum behind the reference (half a step of 1),
+    and the others' share, of which sums may lose any part.  (64 above the reference were 22 u.)"""
+    from paper_2602_24082_b200 import binding as B
+    n = 60
+    rows = [[(1, (n,))]]
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn(n + 1, V, generator=g).clamp(-3, 3)
+    ids = torch.randint(0, V, (n + 1,), generator=g)
+    peak = temperature * torch.linspace(20, 70, n, dtype=torch.float64)
+    x[torch.arange(n), ids[1:]] = peak.float()
+    x = x.to(TYPES[kind][0]).cuda()
+    plan = _plan(rows)
+    logp, stats = B.pp_token_logp(plan, x, ids.cuda(), temperature)
+    temp = float(np.float32(temperature))
+    x64, y = _f64(x)[:n], ids[1:].numpy()
+    own = x64[np.arange(n), y]
+    others = np.exp((x64 - own[:, None]) / temp)
+    others[np.arange(n), y] = 0
+    want = -np.log1p(others.sum(1))
+    err = np.abs(_f64(logp)[1:] - want)
+    assert (err <= U * 8.3 + np.minimum(-want, U * 600)).all(), (err / U).max()
+    # the token's own column: g (1 - p) / temperature
+    d = B.pp_token_logp_bwd(plan, x, ids.cuda(), logp, stats, torch.ones(n + 1, device="cuda"), temperature)
+    got = _f64(d)[np.arange(n), y]
+    tol = (U * 8.5 + np.minimum(-want, U * 600)) / temp + TYPES[kind][1] * -want / temp + TYPES[kind][2]
+    assert (np.abs(got + np.expm1(want) / temp) <= tol).all()
