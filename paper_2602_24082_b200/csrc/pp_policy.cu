@@ -89,7 +89,11 @@ __global__ void __launch_bounds__(kThreads) policy_loss_kernel(PolicyArgs p, int
   if (kTeam == kThreads && parts > 1) cooperative_groups::this_cluster().barrier_arrive();
   const int status = p.header[0];
   const int g = warp_upper(p.grp_resp_off, p.G, x);
-  if (status != kStatusOk) return;   // (a refused plan's offsets may point anywhere)
+  if (status != kStatusOk) {   // (a refused plan's offsets may point anywhere)
+    // who has arrived waits, too.  (Arriving behind this look at the status is 0.2 us later, of 6.9)
+    if (kTeam == kThreads && parts > 1) cooperative_groups::this_cluster().barrier_wait();
+    return;
+  }
   const int seg = g + 1 + x;
   const int a = p.seg_start[seg], b = p.seg_start[seg + 1];
   const int x0 = p.grp_resp_off[g], n = p.grp_resp_off[g + 1] - x0, sp = g + x0;

@@ -204,3 +204,38 @@ def test_calls_of_two_streams_on_one_plan():
                 got[i] = work(*data[i])
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
+
+
+@pytest.mark.parametrize("prompts,responses", [((5, 7), (4, 3, 6)), ((900, 800), (700, 650, 900)), ((3000, 2000), (2100, 1700, 1800))],
+                         ids=["warps", "four_blocks", "eight_blocks"])
+def test_a_refused_plan_leaves_every_output_as_it_was(prompts, responses):
+    """All outputs given, through the C entries, for segments that a warp, a block and clusters of blocks take."""
+    import ctypes
+    from paper_2602_24082_b200 import binding as B
+    T, V = sum(prompts) + sum(responses), 99
+    desc = [np.asarray(a, np.int32) for a in ([0, 1, 2], (prompts[0] + 1,) + prompts[1:], [0, 2, 3], responses)]
+    plan = B.pp_build_plan(tuple(desc), 2, 1, 64, T, desc_on_device=True)
+    f = lambda *shape: torch.full(shape, 7.0, device="cuda")
+    i = lambda *shape: torch.full(shape, 7, dtype=torch.int32, device="cuda")
+    x, t, ids, status, pos = f(T, V), f(T), torch.zeros(T, dtype=torch.int64, device="cuda"), i(2), i(3, T)
+    start, grid = i(1), i(1, 3)
+    logp, stats, d, grad = f(T), f(T, 2), f(T, V), f(T)
+    adv, loss, kl, cut = f(3), f(3), f(3), f(3)
+    q, k = f(T, 2, 64).bfloat16(), f(T, 1, 64).bfloat16()
+
+    class Policy(ctypes.Structure):
+        _fields_ = [("mode", ctypes.c_int32), ("reduction", ctypes.c_int32)] + [(n, ctypes.c_double) for n in "abcde"]
+
+    L, h, p, s = B.lib(), plan.handle, (lambda a: a.data_ptr()), torch.cuda.current_stream().cuda_stream
+    axis = ctypes.create_string_buffer(bytes(32), 32)
+    policy = Policy(2, 0, 0.2, 0.2, 0.1, 1.0, 1e-6)
+    mask = torch.ones(T, dtype=torch.bool, device="cuda")
+    assert L.pp_token_logp(h, p(x), 2, V, V, p(ids), 1, 1.0, p(logp), p(stats), s) == 0
+    assert L.pp_token_logp_bwd(h, p(x), 2, V, V, p(ids), 1, 1.0, p(t), p(stats), p(t), p(d), V, s) == 0
+    assert L.pp_policy_loss(h, ctypes.byref(policy), p(t), p(t), p(t), p(t), p(mask), p(adv), p(loss), p(kl), p(cut), p(grad), s) == 0
+    assert L.pp_position_ids_axes(h, 1, p(start), p(grid), p(pos), p(status), s) == 0
+    assert L.pp_rope_qk_axes(h, p(q), 128, p(k), 64, p(q), 128, p(k), 64, p(pos), 3, axis, 10000.0, 0, s) == 0
+    torch.cuda.synchronize()
+    assert plan.status()[0] in (1, 2)
+    for out in (x, t, logp, stats, d, adv, loss, kl, cut, grad, status, pos, q, k):
+        assert (out == 7).all()
