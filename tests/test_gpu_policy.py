@@ -203,3 +203,21 @@ def test_refusals():
                dict(kl_coef=-1), dict(kl_coef=nan), dict(scale=nan), dict(eps=0), dict(eps=nan)):
         with pytest.raises(B.PPError):
             B.pp_policy_loss(plan, lp, None, None, r, **kw)
+
+
+@pytest.mark.parametrize("mode,reduction,masked", [("normalized", "response", True), ("token", "token", False)])
+@pytest.mark.parametrize("rows", [[[(9, (2000,) * 80)]], [[(9, (500,) * 160)]], [[(9, (700,) * 40)]]],
+                         ids=["four_blocks_of_eight", "one_block_of_four", "four_blocks"])
+def test_parity_where_clusters_would_not_fit_the_chip(rows, mode, reduction, masked):
+    """Long responses, many of them: four blocks for each where eight would be more than four to an SM, and one where
+    four would be."""
+    from paper_2602_24082_b200 import binding as B
+    lp, old, ref, reward, mask = _inputs(rows, mode, 5, masked)
+    kw = dict(clip_low=0.2, clip_high=0.28, kl_coef=0.04, reduction=reduction, scale=0.3)
+    want = P.policy_loss(rows, lp, old, ref, reward, mode=mode, mask=mask, **kw)
+    plan = B.plan_for(W.Workload("policy", rows, 2, 1, 64, seed=0))
+    args = (plan, _cuda(lp), _cuda(old), _cuda(ref), _cuda(reward))
+    got = B.pp_policy_loss(*args, advantage=mode, token_mask=_cuda(mask), **kw)
+    _check(got, want)
+    again = B.pp_policy_loss(*args, advantage=mode, token_mask=_cuda(mask), **kw)
+    assert plan.status() == (0, 0) and all(a is b is None or torch.equal(a, b) for a, b in zip(got, again))
