@@ -104,3 +104,14 @@ def test_sizes_beyond_32_bit_indices(lib, plan):
     assert lib.pp_rope_qk_axes(long, A, 256, 2 * A, 128, 3 * A, 256, 4 * A, 128, A, 3, axis, 10000.0, 0, None) == -2
     assert lib.pp_position_ids_axes(long, 0, None, None, A, A, None) == -2
     assert lib.pp_position_ids_axes(plan, 12, A, A, A, A, None) == -1      # more spans than tokens
+
+
+def test_more_spans_than_32_bit_indices_of_their_sides(lib):
+    """Three int32 sides a span: entries from 2^31 on begin with span 715827883."""
+    w = W.Workload("e", [[(5, (2, 4))]], 4, 2, 64, seed=0)
+    p, keep = B.make_problem(w.descriptors(), 4, 2, 64, 2 ** 31 - 70000)
+    long = ctypes.create_string_buffer(4096)
+    ctypes.memmove(long, ctypes.byref(p), ctypes.sizeof(p))
+    for n in (2 ** 29 + 1, 715827883, 2 ** 30, 2 ** 31 - 70000):
+        assert lib.pp_position_ids_axes(long, n, None, None, A, A, None) == -2
+    assert lib.pp_position_ids_axes(long, 2 ** 29, None, None, A, A, None) == -1       # (no arrays)
