@@ -243,7 +243,7 @@ int pp_preference_loss(const pp_plan* plan, const float* token_logp, const float
  *   in : span_start [num_spans <= T] ascending, span_grid [num_spans][3] (int32; may be NULL without spans).  A span lies
  *        inside one segment (a prompt or a response); spans do not overlap
  *   out: position_ids [3][T] (int32); status [2]: 0 = fine, 1 = a span breaks these rules, and status[1] = the
- *        first such span (the positions of its group's tokens are then undefined)
+ *        first such span (position_ids are then undefined, those of other groups too)
  *
  * Rotary embedding by axes (rotate-half form): frequency i of head_dim / 2 turns by
  * position_ids[axis_of_freq[i]][t] * rope_base^(-2i/D).  axis_of_freq: HOST array of head_dim / 2 entries below

@@ -378,7 +378,8 @@ def pp_position_ids_axes(plan: Plan, span_start: torch.Tensor, span_grid: torch.
     """Packed position ids with a time, a height and a width axis.  Image and video tokens come in
     spans: ``span_start`` [I] their first packed tokens, ascending, ``span_grid`` [I, 3] their (frames, height, width),
     int32 DEVICE tensors.  Returns (position_ids [3, T] int32, status [2] int32); a ``status[0]`` of 1
-    says that span ``status[1]`` does not lie inside one segment or overlaps the one before it."""
+    says that span ``status[1]`` does not lie inside one segment, overlaps the one before it or is not behind it:
+    position_ids are then undefined.  What a call returns shares one allocation."""
     return _step_calls().position_ids_axes(plan.handle, plan.workspace, plan.total_tokens, int(span_start.numel()),
                                            span_start, span_grid, out)
 
@@ -414,7 +415,8 @@ def pp_token_logp(plan: Plan, logits: torch.Tensor, token_ids: torch.Tensor, tem
     """Log-probabilities of the packed response tokens from ``logits`` [T, V] (bf16, fp16 or fp32; adjacent columns)
     under ``token_ids`` [T] (int32 or int64, negative: not learned).  The first token of every response is
     predicted by the prompt's last row.  Returns (token_logp [T], row_stats [T, 2]), both fp32; ``row_stats``
-    is for the backward pass."""
+    is for the backward pass.  They share one allocation, which either keeps alive: a program that keeps token_logp for
+    long gives a tensor of its own, or clones it."""
     return _step_calls().token_logp(plan.handle, plan.workspace, plan.total_tokens, logits, token_ids, temperature,
                                     token_logp, row_stats)
 
@@ -441,7 +443,7 @@ def pp_policy_loss(plan: Plan, token_logp: torch.Tensor, old_token_logp: Optiona
     ("given", "centered" on its group's mean, "normalized" also by the group's standard deviation) or of a token
     ("token", reward [T]).  ``token_mask`` [T] bool.  ``reduction``: mean over a response's tokens ("response") or
     sum ("token"), times ``scale``.  Returns (resp_loss [N], resp_kl [N], resp_clipped [N], advantage [N] or None,
-    d_token_logp [T] or None); the loss is resp_loss.sum()."""
+    d_token_logp [T] or None), which share one allocation; the loss is resp_loss.sum()."""
     if advantage not in _ADVANTAGES:
         raise ValueError(f"advantage: expected one of {', '.join(_ADVANTAGES)}, got {advantage!r}")
     if reduction not in _REDUCTIONS:
