@@ -563,3 +563,21 @@ def test_certain_tokens(V, temperature, kind):
     got = _f64(d)[np.arange(n), y]
     tol = (U * 8.5 + np.minimum(-want, U * 600)) / temp + TYPES[kind][1] * -want / temp + TYPES[kind][2]
     assert (np.abs(got + np.expm1(want) / temp) <= tol).all()
+
+
+@pytest.mark.parametrize("T,V,kind", [(9600, 66001, "fp16"), (9601, 33001, "fp32"), (20000, 40000, "fp32")])
+def test_blocks_that_look_over_several_rows_of_other_types(T, V, kind):
+    from paper_2602_24082_b200 import binding as B
+    rows = [[(T - 310, (200, 7))], [(2, (1, 100))]]
+    g = torch.Generator(device="cuda").manual_seed(0)
+    logits = torch.randn(T, V, generator=g, device="cuda", dtype=TYPES[kind][0])
+    ids = torch.randint(0, V, (T,), generator=g, device="cuda")
+    (a, s), (b, _) = (B.pp_token_logp(_plan(rows, desc_on_device=d), logits, ids) for d in (False, True))
+    assert torch.equal(a, b)
+    r, t = (torch.tensor(x, device="cuda") for x in zip(*P.predictions(rows)))
+    x = logits[r].double()
+    want = torch.log_softmax(x, -1)[torch.arange(len(t), device="cuda"), ids[t]]
+    assert float((a[t].double() - want).abs().max()) < U * (600 + 8 * 12 + 8 * 30)
+    used = torch.zeros(T, dtype=torch.bool, device="cuda")
+    used[r] = True
+    assert not s[~used].any() and torch.equal(s[r, 0].double(), x.amax(1)) and a.count_nonzero() <= len(t)
