@@ -581,3 +581,60 @@ def test_blocks_that_look_over_several_rows_of_other_types(T, V, kind):
     used = torch.zeros(T, dtype=torch.bool, device="cuda")
     used[r] = True
     assert not s[~used].any() and torch.equal(s[r, 0].double(), x.amax(1)) and a.count_nonzero() <= len(t)
+
+
+@pytest.mark.parametrize("n,V,kind,extra", [(129, 300, "bf16", 0), (500, 300, "fp32", 5000), (700, 1000, "fp16", 0), (1500, 40, "bf16", 0),
+                                            (1200, 33000, "bf16", 0), (1100, 130001, "fp32", 0), (3000, 1, "fp32", 0), (3000, 7001, "fp32", 4000)])
+def test_many_responses_to_a_prompt(n, V, kind, extra):
+    """Their first tokens share a row of the gradient; ids that many of them have, some not learned, some beyond the vocabulary."""
+    from paper_2602_24082_b200 import binding as B
+    rows, T = [[(3 + extra, (1, 2) * (n // 2) + (1,) * (n % 2))]], 3 + extra + n // 2 * 3 + n % 2
+    g = torch.Generator(device="cuda").manual_seed(n)
+    logits = torch.randn(T, V, generator=g, device="cuda").to(TYPES[kind][0])
+    ids = (torch.rand(T, generator=g, device="cuda") ** 3 * V).long()          # (the first ones often)
+    ids[torch.rand(T, generator=g, device="cuda") < 0.1] = -1
+    plan = _plan(rows)
+    logp, stats = B.pp_token_logp(plan, logits, ids)
+    grad = torch.randn(T, generator=g, device="cuda")
+    d = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, grad)
+    r = 2 + extra
+    y = torch.tensor([t for row, t in P.predictions(rows) if row == r], device="cuda")
+    assert len(y) == n
+    y = y[ids[y] >= 0]
+    lp = torch.log_softmax(logits[r].double(), 0)
+    assert float((logp[y].double() - lp[ids[y]]).abs().max()) < U * (600 + 8 * 12 + 8 * 30)
+    w, w_abs = (torch.zeros(V, dtype=torch.float64, device="cuda").index_add_(0, ids[y], x) for x in (grad[y].double(), grad[y].double().abs()))
+    want = w - lp.exp() * grad[y].double().sum()
+    # (the sums of the gradients, in 64 bits, are rounded once each: one step of what is subtracted from one another)
+    size = w_abs * -torch.expm1(lp) + lp.exp() * float(grad[y].abs().sum())
+    _, half, tiny = TYPES[kind]
+    err = (d[r].double() - want).abs()
+    assert (err <= half * want.abs() * (1 + 2 * half) + U * (700 + 8 * np.log2(V + 1)) * size + tiny).all()
+    # ids beyond the vocabulary have no column, and what they write to is nobody's
+    ids[y[::2]] += V
+    d2 = B.pp_token_logp_bwd(plan, logits, ids, logp, stats, grad)
+    z = y[1::2]
+    want = torch.zeros(V, dtype=torch.float64, device="cuda").index_add_(0, ids[z], grad[z].double()) - lp.exp() * grad[y].double().sum()
+    assert ((d2[r].double() - want).abs() <= half * want.abs() * (1 + 2 * half) + U * (700 + 8 * np.log2(V + 1)) * size + tiny).all()
+    assert torch.equal(B.pp_token_logp_bwd(plan, logits, ids, logp, stats, grad, d_logits=logits), d2)
+
+
+def test_time_of_many_responses_is_not_their_square():
+    from paper_2602_24082_b200 import binding as B
+    times = []
+    for n in (4096, 32768):
+        rows = [[(3, (1,) * n)]]
+        logits = torch.zeros(n + 3, 500, dtype=torch.bfloat16, device="cuda")
+        ids = torch.arange(n + 3, device="cuda") % 500
+        plan = _plan(rows)
+        logp, stats = B.pp_token_logp(plan, logits, ids)
+        grad, took = torch.ones(n + 3, device="cuda"), []
+        for _ in range(5):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            B.pp_token_logp_bwd(plan, logits, ids, logp, stats, grad)
+            b.record()
+            torch.cuda.synchronize()
+            took.append(a.elapsed_time(b))
+        times.append(min(took))
+    assert times[1] < 24 * times[0]        # (8 times as many: 64 times as long, were it the square)
