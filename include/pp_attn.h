@@ -231,7 +231,7 @@ int pp_preference_loss(const pp_plan* plan, const float* token_logp, const float
  * need only a plan for the same descriptors, are one kernel on `stream`, and take DEVICE
  * pointers; results do not depend on the order in which blocks run.  They leave the plan as it is: calls on one
  * plan may overlap with each other and with the attention.  With a plan that the device has refused
- * (pp_plan_status) they write nothing.  More than 2^31 - 2^16 tokens, a vocabulary beyond 2^30, or more than 2^29
+ * (pp_plan_status) they write nothing.  More than 2^31 - 2^16 tokens, a vocabulary beyond 2^30, or more than 2^24
  * spans, are PP_ERR_UNSUPPORTED.
  *
  * Position ids with a time, a height and a width axis (the paper trains on image prompts, Sec. 4).  A

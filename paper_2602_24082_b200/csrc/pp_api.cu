@@ -426,8 +426,8 @@ int pp_position_ids_axes(const pp_plan* plan, int32_t num_spans, const int32_t* 
   g_last_launches = 0;
   if (!plan || !position_ids || !status || num_spans < 0) return PP_ERR_INVALID_ARG;
   if (num_spans > plan->prob.total_tokens) return PP_ERR_INVALID_ARG;   // (they cannot all be one after the other)
-  // (a span's three sides have 32-bit indices)
-  if (too_long(plan) || num_spans > 1 << 29) return PP_ERR_UNSUPPORTED;
+  // (three sides a span have 32-bit indices, and the time of a group grows with the square of its spans)
+  if (too_long(plan) || num_spans > 1 << 24) return PP_ERR_UNSUPPORTED;
   if (num_spans && (!span_start || !span_grid)) return PP_ERR_INVALID_ARG;
   if (pp::launch_position_ids_axes(plan, num_spans, span_start, span_grid, position_ids, status,
                                    reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess)
