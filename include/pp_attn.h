@@ -251,7 +251,7 @@ int pp_preference_loss(const pp_plan* plan, const float* token_logp, const float
  * is reduced without rounding.  q, k are read and q_out, k_out written, bf16 with the heads
  * of a token side by side ([T][H][D] with strides of *_stride elements between tokens, multiples of 8, at least H * D), so that
  * they may lie in the buffer of a fused projection; in place where the output is the input
- * (same pointer and stride); otherwise they must not overlap.  inverse != 0 turns the other
+ * (same pointer and stride); otherwise an output must not overlap what else is given (PP_ERR_INVALID_ARG where the strides are alike).  inverse != 0 turns the other
  * way, which is the backward pass: dQ and dK in, the gradients of what was rotated out.
  */
 int pp_position_ids_axes(const pp_plan* plan, int32_t num_spans, const int32_t* span_start,
@@ -279,7 +279,8 @@ int pp_rope_qk_axes(const pp_plan* plan, const void* q, int64_t q_stride, const 
  * tokens and of tokens with a negative id do not count), in the logits' type:
  *   d_logits[r][v] = sum over the tokens t that row r predicts of d_token_logp[t] * (1[v = y_t] - p_r(v)) / temperature
  * Every row is written; a row that predicts nothing, or whose tokens' gradients are all zero, is
- * not read and gets zeros.  d_logits may be logits (same pointer and stride).  token_logp and
+ * not read and gets zeros.  d_logits may be logits (same pointer and stride) and must not overlap them
+ * otherwise (PP_ERR_INVALID_ARG where the strides are alike).  token_logp and
  * row_stats are those of the forward call with the same logits, ids and temperature.
  * Both leave what lies between vocab and the stride as it is.  16-byte loads where rows of logits and of
  * d_logits start alike to 16 bytes, element by element otherwise.

@@ -400,7 +400,8 @@ def pp_rope_qk_axes(plan: Plan, q: torch.Tensor, k: torch.Tensor, position_ids: 
                     inverse: bool = False, q_out: Optional[torch.Tensor] = None,
                     k_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Rotary embedding of q [T,Hq,D] and k [T,Hkv,D] by ``position_ids`` [axes, T] int32, in place or into
-    ``q_out`` / ``k_out``; q, k and the outputs may be views of a fused projection's buffer.
+    ``q_out`` / ``k_out``; q, k and the outputs may be views of a fused projection's buffer
+    that do not overlap.
     ``sections``: how many of the D / 2 frequencies each axis has (see ``axis_of_frequency``).
     ``inverse``: the backward pass, on dQ and dK.  Returns (q_out, k_out)."""
     sections = tuple(sections)

@@ -421,6 +421,15 @@ int pp_preference_loss(const pp_plan* plan, const float* token_logp, const float
 // Token indices of the calls around the attention are 32 bits, and are stepped past the last one by a block's width.
 static bool too_long(const pp_plan* plan) { return plan->prob.total_tokens > INT32_MAX - 65536; }
 
+// Whether rows of `wa` bytes from a on and of `wb` from b on, T each, both `stride` bytes apart, have a byte in common.
+// (Side by side in one buffer, as those of a fused projection, they have none.)
+static bool rows_overlap(const void* a, int64_t wa, const void* b, int64_t wb, int64_t stride, int64_t T) {
+  const int64_t apart = reinterpret_cast<intptr_t>(b) - reinterpret_cast<intptr_t>(a), span = (T - 1) * stride;
+  if (apart >= span + wa || -apart >= span + wb) return false;
+  const int64_t d = (apart % stride + stride) % stride;
+  return d < wa || stride - d < wb;
+}
+
 int pp_position_ids_axes(const pp_plan* plan, int32_t num_spans, const int32_t* span_start, const int32_t* span_grid,
                          int32_t* position_ids, int32_t* status, pp_stream_t stream) {
   g_last_launches = 0;
@@ -453,6 +462,13 @@ int pp_rope_qk_axes(const pp_plan* plan, const void* q, int64_t q_stride, const 
   if (q_out == q && q_out_stride != q_stride) return PP_ERR_INVALID_ARG;
   if (k_out == k && k_out_stride != k_stride) return PP_ERR_INVALID_ARG;
   if (q_out == k_out || q_out == k || k_out == q) return PP_ERR_INVALID_ARG;
+  auto on = [&](const void* a, int64_t a_stride, int64_t a_width, const void* b, int64_t b_stride, int64_t b_width) {
+    return a_stride == b_stride && rows_overlap(a, 2 * a_width, b, 2 * b_width, 2 * a_stride, p.total_tokens);
+  };
+  if ((q_out != q && on(q, q_stride, qd, q_out, q_out_stride, qd)) ||
+      (k_out != k && on(k, k_stride, kd, k_out, k_out_stride, kd)) || on(q, q_stride, qd, k_out, k_out_stride, kd) ||
+      on(k, k_stride, kd, q_out, q_out_stride, qd) || on(q_out, q_out_stride, qd, k_out, k_out_stride, kd))
+    return PP_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) ||
       ((q_stride | k_stride | q_out_stride | k_out_stride) & 7))
     return PP_ERR_ALIGNMENT;
@@ -497,6 +513,10 @@ int pp_token_logp_bwd(const pp_plan* plan, const void* logits, int32_t logits_ty
   if (d_logits == logits && d_row_stride != row_stride) return PP_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(row_stats) & 7) return PP_ERR_ALIGNMENT;
   if (reinterpret_cast<uintptr_t>(d_logits) & (logits_type == PP_FP32 ? 3 : 1)) return PP_ERR_ALIGNMENT;
+  const int64_t size = logits_type == PP_FP32 ? 4 : 2;
+  if (d_logits != logits && d_row_stride == row_stride &&
+      rows_overlap(logits, vocab * size, d_logits, vocab * size, row_stride * size, plan->prob.total_tokens))
+    return PP_ERR_INVALID_ARG;
   if (pp::launch_token_logp_bwd(plan, logits, logits_type, row_stride, vocab, token_ids, ids_are_64 != 0, temperature,
                                 token_logp, row_stats, d_token_logp, d_logits, d_row_stride,
                                 reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess)

@@ -115,3 +115,23 @@ def test_more_spans_than_32_bit_indices_of_their_sides(lib):
     for n in (2 ** 24 + 1, 715827883, 2 ** 30, 2 ** 31 - 70000):
         assert lib.pp_position_ids_axes(long, n, None, None, A, A, None) == -2
     assert lib.pp_position_ids_axes(long, 2 ** 24, None, None, A, A, None) == -1       # (no arrays)
+
+
+def test_outputs_that_overlap_their_inputs(lib, plan):
+    """11 tokens.  Rows that share bytes are refused.  Rows side by side in one buffer are not: those calls go on to the
+    check of alignment, which a shift of all by 8 bytes ends."""
+    bwd = lambda x, d, V, stride: lib.pp_token_logp_bwd(plan, x, 0, stride, V, A, 0, 1.0, A, A, A, d, stride, None)
+    x = 1 << 20
+    for shift in (2, 100, 198, 400 - 198, 398, 400 + 20, 4000, 4000 + 198, -2, -198, -398, -4000, -4000 - 198):
+        assert bwd(x, x + shift, 100, 200) == -1, shift
+    axis = ctypes.create_string_buffer(bytes([0, 1, 2] * 10 + [0, 0]), 32)
+    rope = lambda q, k, qo, ko, s: lib.pp_rope_qk_axes(plan, q, s, k, s, qo, s, ko, s, A, 3, axis, 10000.0, 0, None)
+    s, h, far = 640, 128, 1 << 22           # a token of the fused buffer: 10 heads of 64, 128 bytes each; q 4 of them, k 2
+    for args in ((x, x + 4 * h, x + h, far), (x, x + 4 * h, x + 3 * h, far), (x + h, x + 5 * h, x, far), (x, x + 4 * h, far, x + 5 * h),
+                 (x, x + 4 * h, far, x + 3 * h), (x, x + 4 * h, x + 5 * h, far), (x, far, x + 7 * h, far), (far, x, 2 * far, x + 2 * s + h),
+                 (x, x + 4 * h, far, far + 3 * h), (x, x + 4 * h, far + 2 * s * 9 + h, far), (x, far, x + 10 * 2 * s + 3 * h, 3 * far)):
+        assert rope(*args, s) == -1, args
+    # side by side, one after the other, in place: nothing but the alignment is wrong
+    for args in ((x, x + 4 * h, x + 6 * h, far), (x, x + 4 * h, far, x + 6 * h), (x, x + 4 * h, x, x + 4 * h), (x, x + 4 * h, far, far + 4 * h),
+                 (x, far, x + 10 * 2 * s + 4 * h, 3 * far), (far, x, 2 * far, x - 10 * 2 * s - 2 * h)):
+        assert rope(*[a + 8 for a in args], s) == -4, args
