@@ -12,18 +12,18 @@
 // Rows that predict nothing are not read; their gradient is zero.
 //
 // Both passes are bound by HBM: the forward reads a predicting row once, with the running maximum and sum of a
-// softmax, the backward reads and writes it once.  9241 rows of 128256 bf16 columns, 4935 of which predict something: 1.27 GB
-// in 195 us (6.5 TB/s, as a copy), the gradient 3.64 GB in 552 - 576 (6.6 - 6.3, from one B200 to another).  What
-// keeps the forward at the memory's rate is one exponential per element and little else: bf16 at 6.5 TB/s are 11.7
-// elements per clock and SM, of 16 that the special function unit makes (measured busy for 79 %).  The exponential is 2^(c x - K), c = log2(e) /
-// temperature, with a whole number K for reference: K is exact in fp32, so nothing of c x is
-// lost to the rounding of a reference (c m rounded would be off by 2^-24 |c m|, the same for the whole
-// row), and sums of different references are joined by exact powers of two.  K comes from a thread's first elements and
-// stays unless one is 2^8 times as large: a new reference with every new maximum was a branch that some lane of
-// a warp took in nearly every step (with it, and a look at the row's end for every vector, 128 instead of 105 million
-// instructions; under the power limit of a long run, at 1.7 GHz, 219 us instead of 210).  An exponent of up to 8 is rounded
-// to 2^-22; up to 64 it was 2^-19, which of a certain token's log-probability is the whole, and no faster (195
-// us and 210, both).  A thread has four 16-byte vectors on their way while it sums up four (without that 252 us).
+// softmax, the backward reads and writes it once.  9241 rows of 128256 bf16 columns, 4935 of which predict something:
+// 1.27 GB in 195 us (6.5 TB/s, as a copy), the gradient 3.64 GB in 552 - 576 (6.6 - 6.3, from one B200 to another).
+// What keeps the forward at the memory's rate is one exponential per element and little else: bf16 at 6.5 TB/s are
+// 11.7 elements per clock and SM, of 16 that the special function unit makes (measured busy for 79 %).  The
+// exponential is 2^(c x - K), c = log2(e) / temperature, with a whole number K for reference: K is exact in fp32, so
+// nothing of c x is lost to the rounding of a reference (c m rounded would be off by 2^-24 |c m|, the same for the
+// whole row), and sums of different references are joined by exact powers of two.  K comes from a thread's first
+// elements and stays unless one is 2^8 times as large: a new reference with every new maximum was a branch that some
+// lane of a warp took in nearly every step (with it, and a look at the row's end for every vector, 128 instead of 105
+// million instructions; under the power limit of a long run, at 1.7 GHz, 219 us instead of 210).  An exponent of up to
+// 8 is rounded to 2^-22; up to 64 it was 2^-19, which of a certain token's log-probability is the whole, and no faster
+// (195 us and 210, both).  A thread has four 16-byte vectors on their way while it sums up four (without that 252 us).
 // Rows whose values are beyond +-2^19 (a mask of the type's lowest value over everything, say)
 // go through a second pass over exp(x - m).
 #include <cooperative_groups.h>
