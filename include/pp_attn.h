@@ -251,7 +251,8 @@ int pp_preference_loss(const pp_plan* plan, const float* token_logp, const float
  * is reduced without rounding.  q, k are read and q_out, k_out written, bf16 with the heads
  * of a token side by side ([T][H][D] with strides of *_stride elements between tokens, multiples of 8, at least H * D), so that
  * they may lie in the buffer of a fused projection; in place where the output is the input
- * (same pointer and stride); otherwise an output must not overlap what else is given (PP_ERR_INVALID_ARG where the strides are alike).  inverse != 0 turns the other
+ * (same pointer and stride); otherwise an output must not overlap what else is given (PP_ERR_INVALID_ARG where the
+ * strides are alike).  inverse != 0 turns the other
  * way, which is the backward pass: dQ and dK in, the gradients of what was rotated out.
  */
 int pp_position_ids_axes(const pp_plan* plan, int32_t num_spans, const int32_t* span_start,
